@@ -30,6 +30,16 @@
  *                       thread detokenises finished hypotheses while the GPU
  *                       generates the next batch.
  *
+ * Generation by sampling, where rows are no beams of a source, begin and end
+ * at any time and differ in length (not a method of the paper):
+ *
+ *   fs_paged_append     keys and values of new tokens into a paged cache.
+ *   fs_paged_attn       attention of one new token per row over that cache,
+ *                       with shared key-value heads; it can take the token's
+ *                       own key and value and write them.
+ *   fs_token_sample     one token per row by temperature, top-k, top-p and
+ *                       min-p, from given random numbers.
+ *
  * Conventions shared by every entry point
  *   - Pointers named "device" are HIP device memory; the caller owns every
  *     buffer.  The library never allocates, frees or synchronises in these
@@ -56,7 +66,7 @@
  *     other calls on the same workspace.
  *   - Debug mode: with the environment variable FS_VALIDATE=1 set when the
  *     library is first used (or after fs_set_tuning(FS_TUNE_VALIDATE, 1)),
- *     the attention calls copy src_len / prefix_len
+ *     the attention calls copy src_len / prefix_len / kv_len
  *     to the host (synchronising `stream`) and return FS_ERR_INVALID_ARG if
  *     a length lies outside [0, S] instead of clamping it; on a capturing
  *     stream, where that copy cannot run, they return FS_ERR_UNSUPPORTED.
@@ -498,6 +508,144 @@ int fs_postproc_flush(fs_postproc *pp);
 size_t fs_postproc_output(fs_postproc *pp, char *buf, size_t cap);
 double fs_postproc_busy_seconds(fs_postproc *pp);
 void fs_postproc_destroy(fs_postproc *pp);
+
+/*
+ * Paged key-value cache: the keys and values of new tokens are written to the
+ * positions that follow those their rows hold already.
+ *
+ * K and V are [P, Hkv, page, D]: P pages of `page` positions.  Position pos of
+ * row r is slot pos % page of page table[r, pos / page].  Row r's tokens are
+ * n = offsets[r] .. offsets[r+1] - 1 of k and v; with offsets NULL, token r
+ * alone (then N == R).  For every such n and every head h, with
+ * pos = start[r] + n - offsets[r] and pg = table[r, pos / page]:
+ *     K[pg, h, pos % page, :] = k[n, h, :]      V likewise
+ * A token is skipped where pos < 0, pos / page >= cols or pg lies outside
+ * [0, P).  Tokens of no row (before offsets[0], behind offsets[R]) are skipped,
+ * so k and v may be padded.  Nothing else of the cache is written.  Two tokens
+ * that name one slot leave either one's row there.
+ *
+ * Arguments (device pointers except the sizes; strides in elements):
+ *   K, V         dtype, updated in place; both with strides page_stride,
+ *                head_stride and slot_stride between pages, heads and
+ *                positions of a page, and D contiguous elements
+ *   k, v         [N, Hkv, D] dtype, strides token_stride and khead_stride
+ *   table        [R, cols] int32, leading dimension ld_table >= cols
+ *   start        [R] int32, positions each row holds already
+ *   offsets      [R + 1] int32, not decreasing, or NULL
+ *   stream       hipStream_t (NULL = default stream)
+ * Supported: dtype FS_F32 or FS_BF16, D in {16, 32, 64, 128}, any page >= 1,
+ * pointers of K, V, k, v and the strides multiples of 16 bytes, K and V of at
+ * most 64 GiB each, cols * page below 2^31.  Byte copies: exact.
+ * Errors: FS_ERR_INVALID_ARG for negative sizes or strides, page < 1, ld_table
+ * < cols, P < 1, N != R without offsets, null or misaligned pointers, or the
+ * cache overlapping an input (K and V may be interleaved in one allocation);
+ * FS_ERR_UNSUPPORTED for what lies outside the set above; FS_ERR_HIP for a
+ * failed launch.  N, R or Hkv == 0 returns FS_OK with no launch.
+ */
+int fs_paged_append(void *K, void *V, int64_t page_stride, int64_t head_stride, int64_t slot_stride, int P, int page,
+                    const void *k, const void *v, int64_t token_stride, int64_t khead_stride, int N,
+                    const int32_t *table, int ld_table, int cols, const int32_t *start, const int32_t *offsets, int R,
+                    int Hkv, int D, int dtype, void *stream);
+
+/*
+ * Workspace, in bytes, that fs_paged_attn needs for these sizes (the partial
+ * softmax states of rows that several workgroups share, and a counter per row
+ * and head).  Zero-fill it before its first use; a call leaves its counters at
+ * zero again, so any later call that fits may reuse it.  0 for empty problems;
+ * (size_t)-1 for invalid or unsupported sizes.
+ */
+size_t fs_paged_attn_workspace_bytes(int R, int Hq, int Hkv, int page, int cols, int D, int dtype);
+
+/*
+ * Attention of one new token per row over a paged cache (fs_paged_append).
+ *
+ * Query head h of row r reads key-value head g = h / (Hq / Hkv).  With
+ * L = clamp(kv_len[r], 0, cols * page) and pg(j) = table[r, j / page]:
+ *     s_j         = scale * (q[r,h,:] . K[pg(j), g, j % page, :])     j < L
+ *     out[r,h,:]  = sum_j softmax(s)_j * V[pg(j), g, j % page, :]
+ * over the positions whose pg(j) lies in [0, P); out[r,h,:] = 0 where there is
+ * none.  Positions j >= L are never read.
+ *
+ * With k and v (both or neither) position L - 1 is the token itself: its key
+ * and value are taken from k[r,g,:] and v[r,g,:] and also written to the cache
+ * (fs_paged_append's rule; a row of L == 0 or without that page writes nothing
+ * and does not attend it).  kv_len counts the new token.  A page that several
+ * rows' tables share must not be the one that a row writes.
+ *
+ * Arguments (device pointers except the sizes; strides in elements):
+ *   q            [R, Hq, D] dtype, strides q_row_stride and q_head_stride
+ *   K, V, table  as for fs_paged_append; written only with k and v
+ *   kv_len       [R] int32
+ *   k, v         [R, Hkv, D] dtype, strides new_row_stride and
+ *                new_head_stride, or NULL
+ *   scale        factor of the scores (1 / sqrt(D) as a rule), finite
+ *   out          [R, Hq, D] dtype, contiguous
+ *   workspace, workspace_bytes  at least fs_paged_attn_workspace_bytes bytes,
+ *                zero-filled before its first use and written by nothing but
+ *                this call.  Calls that share a workspace must not run
+ *                concurrently; calls of any sizes that fit may follow each
+ *                other, eagerly or replayed from graphs.
+ *   stream       hipStream_t (NULL = default stream)
+ * Supported: fs_paged_append's set; Hq a multiple of Hkv, R * Hq <= 2^24.
+ * Arithmetic: products and sums in fp32 (bf16 weights are taken as a sum of
+ * two bf16 values), one rounding at the end.  The bits depend on the data and
+ * the sizes, never on run or launch.
+ * Errors: those of fs_paged_append; FS_ERR_INVALID_ARG also for Hq not a
+ * multiple of Hkv, one of k and v without the other, a scale that is not
+ * finite, a workspace that is too small or misaligned, or out or the workspace
+ * overlapping another argument.  R or Hq == 0 returns FS_OK with no launch.
+ */
+int fs_paged_attn(const void *q, int64_t q_row_stride, int64_t q_head_stride, void *K, void *V, int64_t page_stride,
+                  int64_t head_stride, int64_t slot_stride, int P, int page, const int32_t *table, int ld_table, int cols,
+                  const int32_t *kv_len, const void *k, const void *v, int64_t new_row_stride, int64_t new_head_stride,
+                  float scale, void *out, int R, int Hq, int Hkv, int D, int dtype, void *workspace,
+                  size_t workspace_bytes, void *stream);
+
+/* Workspace, in bytes, that fs_token_sample needs for these sizes.  Zero-fill
+ * it before its first use; any later call that fits may reuse it.  0 for
+ * R == 0; (size_t)-1 for invalid or unsupported sizes. */
+size_t fs_token_sample_workspace_bytes(int R, int V, int dtype);
+
+/*
+ * One token per row, drawn from the row's logits with a given uniform number.
+ *
+ * With x = logits[r, 0..V-1], T = temperature[r], w_i = exp((x_i - max x) / T)
+ * and the order of falling x, equal logits in the order of their index:
+ *     K  the first top_k[r] tokens of the order (every token where top_k[r]
+ *        lies outside [1, V - 1])
+ *     P  those of K before which, in the order, less than top_p[r] of K's
+ *        weight lies: the first always, all of K where top_p[r] >= 1
+ *     M  those with w_i >= min(min_p[r], 1) (every token where min_p[r] <= 0)
+ * out_token[r] is the first token i of P and M with w_i > 0, in the order of
+ * the indices, at which the running sum of their weights exceeds u[r] times
+ * the whole sum (the last one if none does), and out_logprob[r] the logarithm
+ * of w_i over that sum.  T == 0 takes the largest logit (the smallest index
+ * among equals), with logprob 0.  A NaN top_p or min_p is off.  A row with no
+ * distribution -- a NaN or +inf logit, none above -inf, T negative or NaN --
+ * gives -1 and NaN.  -inf logits (bans) are never drawn.
+ *
+ * Arguments (device pointers except the sizes):
+ *   logits       [R, V] of dtype, leading dimension ld_logits; never written
+ *   u            [R] fp32 in [0, 1)
+ *   temperature, top_p, min_p   [R] fp32, top_k [R] int32; NULL: 1, off, off, off
+ *   out_token    [R] int32;  out_logprob [R] fp32
+ *   workspace, workspace_bytes  at least fs_token_sample_workspace_bytes
+ *                bytes, zero-filled before its first use.  Calls that share
+ *                a workspace must not run concurrently.
+ *   stream       hipStream_t (NULL = default stream)
+ * Supported: dtype FS_F32 or FS_BF16, 1 <= V <= 2^24, R <= 2^20.
+ * Arithmetic: weights and sums in 64 bits; top-p's mass as whole numbers of
+ * 2^-44 of the largest weight (V <= 2^18; 2^(18 - log2 V) times as coarse
+ * above), so a draw depends on the data alone, never on run or launch.
+ * Errors: FS_ERR_INVALID_ARG for negative sizes, V < 1, ld_logits < V, null or
+ * misaligned pointers, a workspace that is too small, or an output or the
+ * workspace overlapping another argument; FS_ERR_UNSUPPORTED for dtype, V or R
+ * outside the set above; FS_ERR_HIP for a failed launch.  R == 0 returns FS_OK
+ * with no launch.
+ */
+int fs_token_sample(const void *logits, int64_t ld_logits, int R, int V, int dtype, const float *u,
+                    const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p,
+                    int32_t *out_token, float *out_logprob, void *workspace, size_t workspace_bytes, void *stream);
 
 #ifdef __cplusplus
 }

@@ -27,7 +27,7 @@ FS_TUNE_VALIDATE = 3
 ATTN_PATHS = {"auto": 0, "split": 1, "whole1": 2, "whole2": 3, "whole4": 4}
 
 # (name, restype, argtypes) for every exported entry point.
-_c_int, _c_size, _vp = ctypes.c_int, ctypes.c_size_t, ctypes.c_void_p
+_c_int, _c_size, _vp, _c_i64 = ctypes.c_int, ctypes.c_size_t, ctypes.c_void_p, ctypes.c_int64
 SIGNATURES = [
     ("fs_abi_version", _c_int, []),
     ("fs_status_string", ctypes.c_char_p, [_c_int]),
@@ -52,6 +52,15 @@ SIGNATURES = [
     ("fs_beam_ancestry_step", _c_int, [_vp, _c_int, _vp] + [_c_int] * 3 + [_vp]),
     ("fs_beam_prefix_attn_indirect", _c_int,
      [_vp] * 7 + [_c_int] * 3 + [_vp] + [_c_int] * 6 + [_vp, _c_size, _vp]),
+    ("fs_paged_append", _c_int,
+     [_vp] * 2 + [_c_i64] * 3 + [_c_int] * 2 + [_vp] * 2 + [_c_i64] * 2 + [_c_int, _vp] + [_c_int] * 2 + [_vp] * 2 +
+     [_c_int] * 4 + [_vp]),
+    ("fs_paged_attn_workspace_bytes", _c_size, [_c_int] * 7),
+    ("fs_paged_attn", _c_int,
+     [_vp] + [_c_i64] * 2 + [_vp] * 2 + [_c_i64] * 3 + [_c_int] * 2 + [_vp] + [_c_int] * 2 + [_vp] * 3 + [_c_i64] * 2 +
+     [ctypes.c_float, _vp] + [_c_int] * 5 + [_vp, _c_size, _vp]),
+    ("fs_token_sample_workspace_bytes", _c_size, [_c_int] * 3),
+    ("fs_token_sample", _c_int, [_vp, _c_i64] + [_c_int] * 3 + [_vp] * 8 + [_c_size, _vp]),
     ("fs_postproc_create", _c_int,
      [ctypes.POINTER(_vp), ctypes.c_char_p, _vp] + [_c_int] * 5 + [ctypes.c_char_p]),
     ("fs_postproc_submit", _c_int, [_vp, _vp, _c_int, _c_int, _c_int, _vp]),

@@ -509,6 +509,207 @@ def cache_reorder(K: torch.Tensor, V: torch.Tensor | None, parent: torch.Tensor,
                                            rows // k, int(k), H, T, tp, D, _DTYPES[K.dtype], _stream_ptr(dev)))
 
 
+# ---- generation by sampling: a paged cache and the draw of a token --------------
+
+def _strided(name: str, t: torch.Tensor, dims: int, dtype=None, device=None) -> None:
+    """A GPU tensor whose rows are contiguous (the other dimensions may be strided)."""
+    if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
+        raise ValueError(f"{name} must be a GPU tensor")
+    if t.dim() != dims:
+        raise ValueError(f"{name} must have {dims} dimensions")
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name} must have contiguous rows (unit stride in its last dimension)")
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}")
+    if device is not None and t.device != device:
+        raise ValueError("all tensors must be on one device")
+
+
+def _int32(name: str, t: torch.Tensor, n: int, device) -> None:
+    _need_cuda(name, t)
+    if t.dtype != torch.int32 or t.shape != (n,) or t.device != device:
+        raise ValueError(f"{name} must be int32 [{n}] on the cache's device")
+
+
+def _paged_cache(K: torch.Tensor, V: torch.Tensor, table: torch.Tensor):
+    """Checks of a paged cache and its table; the table's leading dimension."""
+    _strided("K", K, 4)
+    _strided("V", V, 4, K.dtype, K.device)
+    if K.dtype not in _DTYPES:
+        raise ValueError("K and V must be float32 or bfloat16")
+    if V.shape != K.shape or any(a != b for a, b, n in zip(K.stride(), V.stride(), K.shape) if n > 1):
+        raise ValueError("K and V must have the same shape and strides [P, Hkv, page, D]")
+    _strided("table", table, 2, torch.int32, K.device)
+    return table.stride(0) if table.shape[0] > 1 else table.shape[1]
+
+
+def paged_append(K: torch.Tensor, V: torch.Tensor, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor,
+                 start: torch.Tensor, offsets: torch.Tensor | None = None) -> None:
+    """Keys and values of new tokens into a paged cache, in place.
+
+    K, V [P, Hkv, page, D] float32 or bfloat16 (same strides, contiguous rows);
+    table [R, cols] int32, the pages of each row; start [R] int32, the positions
+    each row holds already; k, v [N, Hkv, D].  Row r's tokens are
+    offsets[r] .. offsets[r+1] - 1 of k and v (``offsets`` [R + 1] int32); without
+    ``offsets`` token r alone.  They go to the positions from start[r] on.
+    Tokens of no row, positions past the table and table entries outside [0, P)
+    are skipped.
+    """
+    st = (_fast or _load_fast()).paged_append(K, V, k, v, table, start, offsets)
+    if st is not None:
+        if st:
+            _N.check(st)
+        return
+    ld = _paged_cache(K, V, table)
+    _strided("k", k, 3, K.dtype, K.device)
+    _strided("v", v, 3, K.dtype, K.device)
+    P, Hkv, page, D = K.shape
+    N, R = k.shape[0], table.shape[0]
+    if k.shape != (N, Hkv, D) or v.shape != k.shape or any(a != b for a, b, n in zip(k.stride(), v.stride(), k.shape) if n > 1):
+        raise ValueError("k and v must be [N, Hkv, D] of the same strides")
+    _int32("start", start, R, K.device)
+    if offsets is not None:
+        _int32("offsets", offsets, R + 1, K.device)
+    with _on(K.device):
+        _N.check(_N.ext().fs_paged_append(
+            K.data_ptr(), V.data_ptr(), K.stride(0), K.stride(1), K.stride(2), P, page, k.data_ptr(), v.data_ptr(),
+            k.stride(0), k.stride(1), N, table.data_ptr(), ld, table.shape[1], start.data_ptr(),
+            None if offsets is None else offsets.data_ptr(), R, Hkv, D, _DTYPES[K.dtype], _stream_ptr(K.device)))
+
+
+def paged_attn_workspace_bytes(R: int, Hq: int, Hkv: int, page: int, cols: int, D: int,
+                               dtype: torch.dtype = torch.bfloat16) -> int:
+    """Bytes of workspace fs_paged_attn needs for these sizes (cols: the table's columns)."""
+    key = ("g", R, Hq, Hkv, page, cols, D, dtype)
+    n = _WS_BYTES.get(key)
+    if n is None:
+        n = _size_or_raise(_native_lib().fs_paged_attn_workspace_bytes(R, Hq, Hkv, page, cols, D, _DTYPES[dtype]))
+        _WS_BYTES[key] = n
+    return n
+
+
+def paged_attn(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, table: torch.Tensor, kv_len: torch.Tensor,
+               out: torch.Tensor | None = None, workspace: torch.Tensor | None = None, k: torch.Tensor | None = None,
+               v: torch.Tensor | None = None, scale: float | None = None) -> torch.Tensor:
+    """Attention of one new token per row over a paged cache.
+
+    q [R, Hq, D] (contiguous rows); K, V [P, Hkv, page, D] and table [R, cols]
+    as for :func:`paged_append`, Hq a multiple of Hkv (query head h reads
+    key-value head h // (Hq // Hkv)); kv_len [R] int32, the positions each row
+    attends.  With ``k`` and ``v`` [R, Hkv, D], position kv_len[r] - 1 is the new
+    token: attended from k and v and written to the cache in the same call.
+    ``scale`` (default 1 / sqrt(D)) multiplies the scores.  Returns out
+    [R, Hq, D] in the input dtype; zeros where a row attends nothing.
+    """
+    if out is not None and workspace is not None:
+        st = (_fast or _load_fast()).paged_attn(q, K, V, table, kv_len, out, workspace, k, v, scale)
+        if st is not None:
+            if st:
+                _N.check(st)
+            return out
+    ld = _paged_cache(K, V, table)
+    _strided("q", q, 3, K.dtype, K.device)
+    P, Hkv, page, D = K.shape
+    R, Hq = q.shape[0], q.shape[1]
+    if q.shape[2] != D or table.shape[0] != R:
+        raise ValueError(f"shape mismatch: q{tuple(q.shape)} K{tuple(K.shape)} table{tuple(table.shape)}")
+    _int32("kv_len", kv_len, R, K.device)
+    if (k is None) != (v is None):
+        raise ValueError("k and v go together")
+    if k is not None:
+        _strided("k", k, 3, K.dtype, K.device)
+        _strided("v", v, 3, K.dtype, K.device)
+        if k.shape != (R, Hkv, D) or v.shape != k.shape or any(
+                a != b for a, b, n in zip(k.stride(), v.stride(), k.shape) if n > 1):
+            raise ValueError("k and v must be [R, Hkv, D] of the same strides")
+    if out is None:
+        out = torch.empty((R, Hq, D), dtype=q.dtype, device=q.device)
+    else:
+        _need_cuda("out", out)
+        if out.shape != q.shape or out.dtype != q.dtype or out.device != q.device:
+            raise ValueError("out must match q in shape, dtype and device")
+    if workspace is None:
+        workspace = new_workspace(paged_attn_workspace_bytes(R, Hq, Hkv, page, table.shape[1], D, q.dtype), q.device)
+    else:
+        _need_cuda("workspace", workspace)
+        if workspace.device != q.device:
+            raise ValueError("all tensors must be on one device")
+    with _on(q.device):
+        _N.check(_N.ext().fs_paged_attn(
+            q.data_ptr(), q.stride(0), q.stride(1), K.data_ptr(), V.data_ptr(), K.stride(0), K.stride(1), K.stride(2), P,
+            page, table.data_ptr(), ld, table.shape[1], kv_len.data_ptr(), None if k is None else k.data_ptr(),
+            None if v is None else v.data_ptr(), 0 if k is None else k.stride(0), 0 if k is None else k.stride(1),
+            out.data_ptr(), R, Hq, Hkv, D, _DTYPES[q.dtype], workspace.data_ptr(),
+            workspace.numel() * workspace.element_size(), _stream_ptr(q.device),
+            (D ** -0.5 if D else 1.0) if scale is None else float(scale)))
+    return out
+
+
+def token_sample_workspace_bytes(R: int, V: int, dtype: torch.dtype = torch.float32) -> int:
+    """Bytes of workspace fs_token_sample needs for these sizes."""
+    key = ("t", R, V, dtype)
+    n = _WS_BYTES.get(key)
+    if n is None:
+        n = _size_or_raise(_native_lib().fs_token_sample_workspace_bytes(R, V, _DTYPES[dtype]))
+        _WS_BYTES[key] = n
+    return n
+
+
+def token_sample(logits: torch.Tensor, u: torch.Tensor, temperature: torch.Tensor | None = None,
+                 top_k: torch.Tensor | None = None, top_p: torch.Tensor | None = None,
+                 min_p: torch.Tensor | None = None, out: tuple | None = None, workspace: torch.Tensor | None = None):
+    """One token per row by temperature, top-k, top-p and min-p, from given random numbers.
+
+    logits [R, V] float32 or bfloat16 (contiguous rows, not modified); u [R]
+    float32 in [0, 1); temperature, top_p, min_p [R] float32 and top_k [R] int32,
+    each row's own settings (None: 1, off, off, off).  Returns (token int32 [R],
+    logprob float32 [R]), the log-probability under the filtered distribution.
+    Temperature 0 takes the largest logit; a row with no distribution gives -1
+    and NaN.  The exact rules are those of fs_token_sample in fastseq_hip.h.
+    ``out`` may pass the two output tensors.
+    """
+    if out is not None and workspace is not None and len(out) == 2:
+        st = (_fast or _load_fast()).token_sample(logits, u, temperature, top_k, top_p, min_p, out[0], out[1], workspace)
+        if st is not None:
+            if st:
+                _N.check(st)
+            return out
+    _strided("logits", logits, 2)
+    if logits.dtype not in _DTYPES:
+        raise ValueError("logits must be float32 or bfloat16")
+    R, V = logits.shape
+    dev = logits.device
+    for name, x, dt in (("u", u, torch.float32), ("temperature", temperature, torch.float32),
+                        ("top_k", top_k, torch.int32), ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32)):
+        if x is None and name != "u":
+            continue
+        _need_cuda(name, x)
+        if x.dtype != dt or x.shape != (R,) or x.device != dev:
+            raise ValueError(f"{name} must be {dt} [R] on the logits' device")
+    if out is None:
+        out = (torch.empty(R, dtype=torch.int32, device=dev), torch.empty(R, dtype=torch.float32, device=dev))
+    else:
+        if len(out) != 2:
+            raise ValueError("out must be (int32, float32) tensors of shape [R]")
+        for o, dt in zip(out, (torch.int32, torch.float32)):
+            _need_cuda("out", o)
+            if o.shape != (R,) or o.dtype != dt or o.device != dev:
+                raise ValueError("out must be (int32, float32) tensors of shape [R]")
+    if workspace is None:
+        workspace = new_workspace(token_sample_workspace_bytes(R, V, logits.dtype), dev)
+    else:
+        _need_cuda("workspace", workspace)
+        if workspace.device != dev:
+            raise ValueError("all tensors must be on one device")
+    ptr = lambda x: None if x is None else x.data_ptr()
+    with _on(dev):
+        _N.check(_N.ext().fs_token_sample(
+            logits.data_ptr(), logits.stride(0) if R > 1 else V, R, V, _DTYPES[logits.dtype], u.data_ptr(),
+            ptr(temperature), ptr(top_k), ptr(top_p), ptr(min_p), out[0].data_ptr(), out[1].data_ptr(),
+            workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_ptr(dev)))
+    return out
+
+
 class PostProcessor:
     """Asynchronous post-processing of finished hypotheses (Section 4.3).
 

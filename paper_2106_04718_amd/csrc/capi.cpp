@@ -11,6 +11,7 @@
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
+#include <limits>
 #include <mutex>
 #include <string>
 #include <vector>
@@ -681,6 +682,265 @@ int fs_cache_reorder(void *K, void *V, const int32_t *parent, int B, int k, int 
         return fail(FS_ERR_INVALID_ARG, "parent overlaps the cache");
     hipError_t e = fs::launch_cache_reorder(K, V, parent, B, k, H, T, t, D, esize, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(e, "fs_cache_reorder launch");
+    return FS_OK;
+}
+
+}  // extern "C"
+
+namespace {
+
+// ---- the paged cache -------------------------------------------------------
+
+// Bytes from the first to the last element of a strided array of `rows` of D
+// contiguous elements (strides in elements, sizes >= 1); -1 past 2^62.
+long long extent(long long n0, long long s0, long long n1, long long s1, long long n2, long long s2, int D, size_t esize) {
+    const __int128 e = ((__int128)(n0 - 1) * s0 + (__int128)(n1 - 1) * s1 + (__int128)(n2 - 1) * s2 + D) * (int)esize;
+    return e > ((__int128)1 << 62) ? -1 : (long long)e;
+}
+
+// What paged_append and paged_attn ask of the cache and its table; the extent
+// of K and of V in bytes.  Not called for empty problems.
+int check_paged(const void *K, const void *V, int64_t page_stride, int64_t head_stride, int64_t slot_stride, int P,
+                int page, const int32_t *table, int ld_table, int cols, int R, int Hkv, int D, int dtype,
+                size_t *kv_bytes, size_t *table_bytes)
+{
+    const size_t esize = dtype == FS_BF16 ? 2 : 4;
+    if (P < 1) return fail(FS_ERR_INVALID_ARG, "a cache of P=%d pages", P);
+    if (!K || !V || (cols > 0 && !table))
+        return fail(FS_ERR_INVALID_ARG, "null pointer (K=%p V=%p table=%p)", K, V, (const void *)table);
+    if (!aligned(K, 16) || !aligned(V, 16)) return fail(FS_ERR_INVALID_ARG, "K and V must be 16-byte aligned");
+    if (!aligned(table, 4)) return fail(FS_ERR_INVALID_ARG, "table must be 4-byte aligned");
+    if (page_stride < 0 || head_stride < 0 || slot_stride < 0)
+        return fail(FS_ERR_INVALID_ARG, "negative stride of the cache");
+    const int64_t per16 = (int64_t)(16 / esize);
+    if ((P > 1 && page_stride % per16) || (Hkv > 1 && head_stride % per16) || (page > 1 && slot_stride % per16))
+        return fail(FS_ERR_INVALID_ARG, "the cache's strides must be multiples of 16 bytes");
+    const long long e = extent(P, page_stride, Hkv, head_stride, page, slot_stride, D, esize);
+    if (e < 0 || e > (64ll << 30)) return fail(FS_ERR_UNSUPPORTED, "K and V may span at most 64 GiB each");
+    if ((long long)cols * page > INT_MAX)
+        return fail(FS_ERR_UNSUPPORTED, "a table of %d pages of %d positions exceeds 2^31 positions", cols, page);
+    *kv_bytes = (size_t)e;
+    *table_bytes = cols > 0 ? ((size_t)(R - 1) * ld_table + cols) * 4 : 0;
+    return FS_OK;
+}
+
+int check_paged_sizes(int R, int Hkv, int P, int page, int ld_table, int cols, int D, int dtype) {
+    if (R < 0 || Hkv < 0 || P < 0 || ld_table < 0 || cols < 0 || D < 0)
+        return fail(FS_ERR_INVALID_ARG, "negative size (R=%d Hkv=%d P=%d ld_table=%d cols=%d D=%d)", R, Hkv, P, ld_table,
+                    cols, D);
+    if (page < 1) return fail(FS_ERR_INVALID_ARG, "page=%d < 1", page);
+    if (ld_table < cols) return fail(FS_ERR_INVALID_ARG, "ld_table=%d < cols=%d", ld_table, cols);
+    if (dtype != FS_F32 && dtype != FS_BF16) return fail(FS_ERR_UNSUPPORTED, "dtype %d is not FS_F32 or FS_BF16", dtype);
+    if (!supported_d(D)) return fail(FS_ERR_UNSUPPORTED, "head dim D=%d not in {16,32,64,128}", D);
+    return FS_OK;
+}
+
+int check_paged_attn_sizes(int R, int Hq, int Hkv, int page, int cols, int D, int dtype) {
+    if (Hq < 0) return fail(FS_ERR_INVALID_ARG, "negative size (Hq=%d)", Hq);
+    const int st = check_paged_sizes(R, Hkv, 1, page, cols, cols, D, dtype);
+    if (st != FS_OK) return st;
+    if (Hkv == 0 ? Hq != 0 : Hq % Hkv != 0)
+        return fail(FS_ERR_INVALID_ARG, "Hq=%d is not a multiple of Hkv=%d", Hq, Hkv);
+    if ((long long)R * Hq > (1 << 24)) return fail(FS_ERR_UNSUPPORTED, "R*Hq=%lld exceeds 2^24", (long long)R * Hq);
+    if ((long long)cols * page > INT_MAX)
+        return fail(FS_ERR_UNSUPPORTED, "a table of %d pages of %d positions exceeds 2^31 positions", cols, page);
+    return FS_OK;
+}
+
+fs::PagedCache paged_cache(void *K, void *V, int64_t page_stride, int64_t head_stride, int64_t slot_stride, int P,
+                           int page, const int32_t *table, int ld_table, int cols, size_t esize)
+{
+    const long long e = (long long)esize;
+    return fs::PagedCache{static_cast<unsigned char *>(K), static_cast<unsigned char *>(V), page_stride * e,
+                          head_stride * e, slot_stride * e, P, page, table, ld_table, cols};
+}
+
+}  // namespace
+
+extern "C" {
+
+int fs_paged_append(void *K, void *V, int64_t page_stride, int64_t head_stride, int64_t slot_stride, int P, int page,
+                    const void *k, const void *v, int64_t token_stride, int64_t khead_stride, int N,
+                    const int32_t *table, int ld_table, int cols, const int32_t *start, const int32_t *offsets, int R,
+                    int Hkv, int D, int dtype, void *stream)
+{
+    g_last_error.clear();
+    int st = check_paged_sizes(R, Hkv, P, page, ld_table, cols, D, dtype);
+    if (st != FS_OK) return st;
+    if (N < 0) return fail(FS_ERR_INVALID_ARG, "negative size (N=%d)", N);
+    if (!offsets && N != R) return fail(FS_ERR_INVALID_ARG, "N=%d tokens for R=%d rows without offsets", N, R);
+    if (N == 0 || R == 0 || Hkv == 0) return FS_OK;
+    const size_t esize = dtype == FS_BF16 ? 2 : 4;
+    size_t kv_bytes = 0, table_bytes = 0;
+    if ((st = check_paged(K, V, page_stride, head_stride, slot_stride, P, page, table, ld_table, cols, R, Hkv, D, dtype,
+                          &kv_bytes, &table_bytes)) != FS_OK)
+        return st;
+    if (!k || !v || !start) return fail(FS_ERR_INVALID_ARG, "null pointer (k=%p v=%p start=%p)", k, v, (const void *)start);
+    if (!aligned(k, 16) || !aligned(v, 16)) return fail(FS_ERR_INVALID_ARG, "k and v must be 16-byte aligned");
+    if (!aligned(start, 4) || !aligned(offsets, 4)) return fail(FS_ERR_INVALID_ARG, "start and offsets must be 4-byte aligned");
+    if (token_stride < 0 || khead_stride < 0) return fail(FS_ERR_INVALID_ARG, "negative stride of k and v");
+    const int64_t per16 = (int64_t)(16 / esize);
+    if ((N > 1 && token_stride % per16) || (Hkv > 1 && khead_stride % per16))
+        return fail(FS_ERR_INVALID_ARG, "the strides of k and v must be multiples of 16 bytes");
+    const long long new_bytes = extent(N, token_stride, Hkv, khead_stride, 1, 0, D, esize);
+    if (new_bytes < 0) return fail(FS_ERR_UNSUPPORTED, "the strides of k and v are too large");
+    if ((long long)N * Hkv * (D * (int)esize / 16) > (long long)INT_MAX * 128)
+        return fail(FS_ERR_UNSUPPORTED, "too many tokens for one launch (N=%d Hkv=%d D=%d)", N, Hkv, D);
+    for (const void *c : {(const void *)K, (const void *)V})
+        if (overlaps(c, kv_bytes, k, new_bytes) || overlaps(c, kv_bytes, v, new_bytes) ||
+            overlaps(c, kv_bytes, table, table_bytes) || overlaps(c, kv_bytes, start, (size_t)R * 4) ||
+            overlaps(c, kv_bytes, offsets, offsets ? ((size_t)R + 1) * 4 : 0))
+            return fail(FS_ERR_INVALID_ARG, "the cache overlaps an input");
+    const fs::PagedCache c = paged_cache(K, V, page_stride, head_stride, slot_stride, P, page, table, ld_table, cols, esize);
+    hipError_t e = fs::launch_paged_append(c, k, v, token_stride * (long long)esize, khead_stride * (long long)esize, N,
+                                           start, offsets, R, Hkv, D * (int)esize, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "fs_paged_append launch");
+    return FS_OK;
+}
+
+size_t fs_paged_attn_workspace_bytes(int R, int Hq, int Hkv, int page, int cols, int D, int dtype) {
+    g_last_error.clear();
+    if (check_paged_attn_sizes(R, Hq, Hkv, page, cols, D, dtype) != FS_OK) return (size_t)-1;
+    if (R == 0 || Hq == 0) return 0;
+    return fs::paged_attn_workspace_bytes(R, Hq, Hkv, page, cols, D);
+}
+
+int fs_paged_attn(const void *q, int64_t q_row_stride, int64_t q_head_stride, void *K, void *V, int64_t page_stride,
+                  int64_t head_stride, int64_t slot_stride, int P, int page, const int32_t *table, int ld_table, int cols,
+                  const int32_t *kv_len, const void *k, const void *v, int64_t new_row_stride, int64_t new_head_stride,
+                  float scale, void *out, int R, int Hq, int Hkv, int D, int dtype, void *workspace,
+                  size_t workspace_bytes, void *stream)
+{
+    g_last_error.clear();
+    int st = check_paged_sizes(R, Hkv, P, page, ld_table, cols, D, dtype);
+    if (st != FS_OK) return st;
+    if ((st = check_paged_attn_sizes(R, Hq, Hkv, page, cols, D, dtype)) != FS_OK) return st;
+    if (!(scale > -std::numeric_limits<float>::infinity() && scale < std::numeric_limits<float>::infinity()))
+        return fail(FS_ERR_INVALID_ARG, "scale is not finite");
+    if (R == 0 || Hq == 0) return FS_OK;
+    const size_t esize = dtype == FS_BF16 ? 2 : 4;
+    size_t kv_bytes = 0, table_bytes = 0;
+    if ((st = check_paged(K, V, page_stride, head_stride, slot_stride, P, page, table, ld_table, cols, R, Hkv, D, dtype,
+                          &kv_bytes, &table_bytes)) != FS_OK)
+        return st;
+    if (!q || !out || !kv_len) return fail(FS_ERR_INVALID_ARG, "null pointer (q=%p out=%p kv_len=%p)", q, out,
+                                           (const void *)kv_len);
+    if ((k == nullptr) != (v == nullptr)) return fail(FS_ERR_INVALID_ARG, "k and v go together (k=%p v=%p)", k, v);
+    if (!aligned(q, 16) || !aligned(out, 16) || !aligned(k, 16) || !aligned(v, 16))
+        return fail(FS_ERR_INVALID_ARG, "q, k, v and out must be 16-byte aligned");
+    if (!aligned(kv_len, 4)) return fail(FS_ERR_INVALID_ARG, "kv_len must be 4-byte aligned");
+    if (q_row_stride < 0 || q_head_stride < 0 || (k && (new_row_stride < 0 || new_head_stride < 0)))
+        return fail(FS_ERR_INVALID_ARG, "negative stride of q, k or v");
+    const int64_t per16 = (int64_t)(16 / esize);
+    if ((R > 1 && q_row_stride % per16) || (Hq > 1 && q_head_stride % per16) ||
+        (k && ((R > 1 && new_row_stride % per16) || (Hkv > 1 && new_head_stride % per16))))
+        return fail(FS_ERR_INVALID_ARG, "the strides of q, k and v must be multiples of 16 bytes");
+    const long long q_bytes = extent(R, q_row_stride, Hq, q_head_stride, 1, 0, D, esize);
+    const long long new_bytes = k ? extent(R, new_row_stride, Hkv, new_head_stride, 1, 0, D, esize) : 0;
+    if (q_bytes < 0 || new_bytes < 0) return fail(FS_ERR_UNSUPPORTED, "the strides of q, k and v are too large");
+    const size_t out_bytes = (size_t)R * Hq * D * esize;
+    if (overlaps(out, out_bytes, q, q_bytes) || overlaps(out, out_bytes, K, kv_bytes) ||
+        overlaps(out, out_bytes, V, kv_bytes) || overlaps(out, out_bytes, table, table_bytes) ||
+        overlaps(out, out_bytes, kv_len, (size_t)R * 4) || overlaps(out, out_bytes, k, new_bytes) ||
+        overlaps(out, out_bytes, v, new_bytes))
+        return fail(FS_ERR_INVALID_ARG, "out overlaps an input");
+    if (k)
+        for (const void *c : {(const void *)K, (const void *)V})
+            if (overlaps(c, kv_bytes, k, new_bytes) || overlaps(c, kv_bytes, v, new_bytes) ||
+                overlaps(c, kv_bytes, q, q_bytes) || overlaps(c, kv_bytes, table, table_bytes) ||
+                overlaps(c, kv_bytes, kv_len, (size_t)R * 4))
+                return fail(FS_ERR_INVALID_ARG, "the cache overlaps an input");
+    const size_t need = fs::paged_attn_workspace_bytes(R, Hq, Hkv, page, cols, D);
+    if (workspace_bytes < need || !workspace)
+        return fail(FS_ERR_INVALID_ARG, "workspace of %zu bytes at %p; %zu bytes needed", workspace_bytes, workspace, need);
+    if (!aligned(workspace, 16)) return fail(FS_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
+    if (overlaps(workspace, need, q, q_bytes) || overlaps(workspace, need, K, kv_bytes) ||
+        overlaps(workspace, need, V, kv_bytes) || overlaps(workspace, need, table, table_bytes) ||
+        overlaps(workspace, need, kv_len, (size_t)R * 4) || overlaps(workspace, need, k, new_bytes) ||
+        overlaps(workspace, need, v, new_bytes) || overlaps(workspace, need, out, out_bytes))
+        return fail(FS_ERR_INVALID_ARG, "workspace overlaps an argument");
+
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (validate_mode() && (st = validate_lengths(kv_len, R, cols * page, s, "kv_len")) != FS_OK) return st;
+    fs::PagedAttn a{};
+    a.cache = paged_cache(K, V, page_stride, head_stride, slot_stride, P, page, table, ld_table, cols, esize);
+    const long long e = (long long)esize;
+    a.q = static_cast<const unsigned char *>(q), a.q_row_bytes = q_row_stride * e, a.q_head_bytes = q_head_stride * e;
+    a.kv_len = kv_len;
+    a.k = static_cast<const unsigned char *>(k), a.v = static_cast<const unsigned char *>(v);
+    a.new_row_bytes = new_row_stride * e, a.new_head_bytes = new_head_stride * e;
+    a.out = static_cast<unsigned char *>(out);
+    a.R = R, a.Hq = Hq, a.Hkv = Hkv, a.scale = scale;
+    a.workspace = static_cast<unsigned char *>(workspace);
+    hipError_t err = fs::launch_paged_attn(a, D, dtype == FS_BF16, s);
+    if (err != hipSuccess) return hip_fail(err, "fs_paged_attn launch");
+    return FS_OK;
+}
+
+}  // extern "C"
+
+namespace {
+
+int check_sample_sizes(int R, int V, int dtype) {
+    if (R < 0 || V < 0) return fail(FS_ERR_INVALID_ARG, "negative size (R=%d V=%d)", R, V);
+    if (dtype != FS_F32 && dtype != FS_BF16) return fail(FS_ERR_UNSUPPORTED, "dtype %d is not FS_F32 or FS_BF16", dtype);
+    if (V < 1) return fail(FS_ERR_INVALID_ARG, "vocabulary V=%d < 1", V);
+    if (V > (1 << 24)) return fail(FS_ERR_UNSUPPORTED, "vocabulary V=%d exceeds 2^24", V);
+    if (R > (1 << 20)) return fail(FS_ERR_UNSUPPORTED, "R=%d rows exceed 2^20", R);
+    return FS_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t fs_token_sample_workspace_bytes(int R, int V, int dtype) {
+    g_last_error.clear();
+    if (check_sample_sizes(R, V, dtype) != FS_OK) return (size_t)-1;
+    if (R == 0) return 0;
+    return fs::token_sample_workspace_bytes(R, V, dtype == FS_BF16 ? 2 : 4);
+}
+
+int fs_token_sample(const void *logits, int64_t ld_logits, int R, int V, int dtype, const float *u,
+                    const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p,
+                    int32_t *out_token, float *out_logprob, void *workspace, size_t workspace_bytes, void *stream)
+{
+    g_last_error.clear();
+    int st = check_sample_sizes(R, V, dtype);
+    if (st != FS_OK) return st;
+    if (ld_logits < 0 || (R > 1 && ld_logits < V))
+        return fail(FS_ERR_INVALID_ARG, "ld_logits=%lld < V=%d", (long long)ld_logits, V);
+    if (R == 0) return FS_OK;
+    if (ld_logits > (1ll << 40)) return fail(FS_ERR_UNSUPPORTED, "ld_logits=%lld is too large", (long long)ld_logits);
+    const size_t esize = dtype == FS_BF16 ? 2 : 4, rows = (size_t)R * 4;
+    if (!logits || !u || !out_token || !out_logprob)
+        return fail(FS_ERR_INVALID_ARG, "null pointer (logits=%p u=%p outputs=%p %p)", logits, (const void *)u,
+                    (void *)out_token, (void *)out_logprob);
+    const void *params[5] = {u, temperature, top_k, top_p, min_p};
+    if (!aligned(logits, esize)) return fail(FS_ERR_INVALID_ARG, "logits must be aligned to their elements");
+    bool ok = aligned(out_token, 4) && aligned(out_logprob, 4);
+    for (const void *p : params) ok = ok && aligned(p, 4);
+    if (!ok) return fail(FS_ERR_INVALID_ARG, "arrays must be 4-byte aligned");
+    const size_t lg_bytes = ((size_t)(R - 1) * (size_t)ld_logits + V) * esize;
+    const size_t need = fs::token_sample_workspace_bytes(R, V, (int)esize);
+    if (workspace_bytes < need || !workspace)
+        return fail(FS_ERR_INVALID_ARG, "workspace of %zu bytes at %p; %zu bytes needed", workspace_bytes, workspace, need);
+    if (!aligned(workspace, 16)) return fail(FS_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
+    const void *outs[2] = {out_token, out_logprob};
+    for (const void *o : outs) {
+        if (overlaps(o, rows, logits, lg_bytes)) return fail(FS_ERR_INVALID_ARG, "an output overlaps an input");
+        for (const void *p : params)
+            if (overlaps(o, rows, p, p ? rows : 0)) return fail(FS_ERR_INVALID_ARG, "an output overlaps an input");
+        if (overlaps(workspace, need, o, rows)) return fail(FS_ERR_INVALID_ARG, "workspace overlaps an argument");
+    }
+    if (overlaps(out_token, rows, out_logprob, rows)) return fail(FS_ERR_INVALID_ARG, "outputs overlap");
+    if (overlaps(workspace, need, logits, lg_bytes)) return fail(FS_ERR_INVALID_ARG, "workspace overlaps an argument");
+    for (const void *p : params)
+        if (overlaps(workspace, need, p, p ? rows : 0)) return fail(FS_ERR_INVALID_ARG, "workspace overlaps an argument");
+    fs::TokenSample a{logits, ld_logits, R, V, u, temperature, top_k, top_p, min_p, out_token, out_logprob,
+                      static_cast<unsigned char *>(workspace)};
+    hipError_t e = fs::launch_token_sample(a, dtype == FS_BF16, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "fs_token_sample launch");
     return FS_OK;
 }
 

@@ -109,4 +109,54 @@ hipError_t launch_cache_reorder(void *K, void *V, const int32_t *parent, int B, 
 hipError_t launch_ancestry_step(int32_t *anc, int ld, const int32_t *parent, int B, int k, int t,
                                 hipStream_t stream);
 
+// A paged key-value cache: K and V [P, Hkv, page, D] with the same strides (in
+// bytes, rows of D contiguous elements) and the table [R, cols] of the pages
+// that hold the rows' positions.
+struct PagedCache {
+    unsigned char *K, *V;
+    long long page_bytes, head_bytes, slot_bytes;
+    int pages, page;
+    const int32_t *table;
+    int ld_table, cols;
+};
+
+// Tokens n < N (key and value rows of row_bytes, a multiple of 16) to the
+// positions that follow start[r] in their rows; offsets null: token n is row n's.
+hipError_t launch_paged_append(const PagedCache &cache, const void *k, const void *v, long long token_bytes,
+                               long long khead_bytes, int N, const int32_t *start, const int32_t *offsets, int R, int Hkv,
+                               int row_bytes, hipStream_t stream);
+
+// Attention of one new token per row.  With k (and v), position kv_len[r] - 1
+// is the new token: it is read from k, v and written to the cache.
+struct PagedAttn {
+    PagedCache cache;
+    const unsigned char *q;
+    long long q_row_bytes, q_head_bytes;
+    const int32_t *kv_len;
+    const unsigned char *k, *v;
+    long long new_row_bytes, new_head_bytes;
+    unsigned char *out;   // [R, Hq, D], contiguous
+    int R, Hq, Hkv;
+    float scale;
+    unsigned char *workspace;
+};
+size_t paged_attn_workspace_bytes(int R, int Hq, int Hkv, int page, int cols, int D);
+hipError_t launch_paged_attn(const PagedAttn &a, int D, bool bf16, hipStream_t stream);
+
+// One token per row of logits [R, V] (leading dimension ld).  A null parameter
+// array means that its filter is off.
+struct TokenSample {
+    const void *logits;
+    long long ld;
+    int R, V;
+    const float *u, *temperature;
+    const int32_t *top_k;
+    const float *top_p, *min_p;
+    int32_t *token;
+    float *logprob;
+    unsigned char *workspace;
+};
+size_t token_sample_workspace_bytes(int R, int V, int esize);
+hipError_t launch_token_sample(const TokenSample &a, bool bf16, hipStream_t stream);
+
 }  // namespace fs

@@ -17,7 +17,7 @@
 
 /* Convert args[0..n) into unsigned 64-bit values (pointers, sizes) or
  * signed ints; the format string holds one letter per argument:
- * 'p' pointer / size_t, 'i' int. */
+ * 'p' pointer, size_t or stride, 'i' int. */
 static int unpack(PyObject *const *args, Py_ssize_t nargs, const char *fmt, unsigned long long *u, int *v) {
     Py_ssize_t n = (Py_ssize_t)strlen(fmt);
     if (nargs != n) {
@@ -127,6 +127,44 @@ static PyObject *py_beam_prefix_attn_indirect(PyObject *self, PyObject *const *a
     return PyLong_FromLong(st);
 }
 
+static PyObject *py_paged_append(PyObject *self, PyObject *const *args, Py_ssize_t nargs) {
+    unsigned long long u[22];
+    int v[22];
+    (void)self;
+    if (unpack(args, nargs, "pppppiippppipiippiiiip", u, v)) return NULL;
+    int st = fs_paged_append(PTR(0), PTR(1), (int64_t)u[2], (int64_t)u[3], (int64_t)u[4], v[5], v[6], PTR(7), PTR(8),
+                             (int64_t)u[9], (int64_t)u[10], v[11], (const int32_t *)PTR(12), v[13], v[14],
+                             (const int32_t *)PTR(15), (const int32_t *)PTR(16), v[17], v[18], v[19], v[20], PTR(21));
+    return PyLong_FromLong(st);
+}
+
+/* scale, a C float, is passed after the arguments that unpack() takes */
+static PyObject *py_paged_attn(PyObject *self, PyObject *const *args, Py_ssize_t nargs) {
+    unsigned long long u[27];
+    int v[27];
+    (void)self;
+    if (nargs != 28) return PyErr_Format(PyExc_TypeError, "expected 28 arguments, got %zd", nargs);
+    if (unpack(args, 27, "ppppppppiipiipppppp" "iiiii" "ppp", u, v)) return NULL;
+    const double scale = PyFloat_AsDouble(args[27]);
+    if (PyErr_Occurred()) return NULL;
+    int st = fs_paged_attn(PTR(0), (int64_t)u[1], (int64_t)u[2], PTR(3), PTR(4), (int64_t)u[5], (int64_t)u[6],
+                           (int64_t)u[7], v[8], v[9], (const int32_t *)PTR(10), v[11], v[12], (const int32_t *)PTR(13),
+                           PTR(14), PTR(15), (int64_t)u[16], (int64_t)u[17], (float)scale, PTR(18), v[19], v[20], v[21],
+                           v[22], v[23], PTR(24), (size_t)u[25], PTR(26));
+    return PyLong_FromLong(st);
+}
+
+static PyObject *py_token_sample(PyObject *self, PyObject *const *args, Py_ssize_t nargs) {
+    unsigned long long u[15];
+    int v[15];
+    (void)self;
+    if (unpack(args, nargs, "ppiiipppppppppp", u, v)) return NULL;
+    int st = fs_token_sample(PTR(0), (int64_t)u[1], v[2], v[3], v[4], (const float *)PTR(5), (const float *)PTR(6),
+                             (const int32_t *)PTR(7), (const float *)PTR(8), (const float *)PTR(9), (int32_t *)PTR(10),
+                             (float *)PTR(11), PTR(12), (size_t)u[13], PTR(14));
+    return PyLong_FromLong(st);
+}
+
 static PyObject *py_last_error(PyObject *self, PyObject *unused) {
     (void)self;
     (void)unused;
@@ -153,6 +191,16 @@ static PyMethodDef methods[] = {
      "fs_beam_ancestry_step(anc, ld_anc, parent, B, k, t, stream)"},
     {"fs_beam_prefix_attn_indirect", (PyCFunction)(void (*)(void))py_beam_prefix_attn_indirect, METH_FASTCALL,
      "fs_beam_prefix_attn_indirect(q, Kp, Vp, prefix_len, Kt, Vt, anc, ld_anc, T, t, out, B, k, H, N, D, dtype, "
+     "workspace, workspace_bytes, stream)"},
+    {"fs_paged_append", (PyCFunction)(void (*)(void))py_paged_append, METH_FASTCALL,
+     "fs_paged_append(K, V, page_stride, head_stride, slot_stride, P, page, k, v, token_stride, khead_stride, N, table, "
+     "ld_table, cols, start, offsets, R, Hkv, D, dtype, stream)"},
+    {"fs_paged_attn", (PyCFunction)(void (*)(void))py_paged_attn, METH_FASTCALL,
+     "fs_paged_attn(q, q_row_stride, q_head_stride, K, V, page_stride, head_stride, slot_stride, P, page, table, "
+     "ld_table, cols, kv_len, k, v, new_row_stride, new_head_stride, out, R, Hq, Hkv, D, dtype, workspace, "
+     "workspace_bytes, stream, scale)"},
+    {"fs_token_sample", (PyCFunction)(void (*)(void))py_token_sample, METH_FASTCALL,
+     "fs_token_sample(logits, ld_logits, R, V, dtype, u, temperature, top_k, top_p, min_p, out_token, out_logprob, "
      "workspace, workspace_bytes, stream)"},
     {"fs_last_error", py_last_error, METH_NOARGS, "fs_last_error() -> str"},
     {NULL, NULL, 0, NULL},

@@ -16,6 +16,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <climits>
+#include <cmath>
 
 #include "fastseq_hip.h"
 
@@ -281,6 +282,102 @@ PyObject *ancestry_step(PyObject *, PyObject *const *a, Py_ssize_t n) {
                                                  (int)(anc.size(0) / k), (int)k, (int)t, s));
 }
 
+// A tensor argument that may be None (then null), else as Args::tensor.
+const at::Tensor *optional(Args &g, int i) { return g.a[i] == Py_None ? nullptr : g.tensor(i); }
+template <typename T>
+T *data(const at::Tensor *t) { return t ? static_cast<T *>(t->data_ptr()) : nullptr; }
+// contiguous rows, the other dimensions as they are
+bool rows_of(const at::Tensor &t, int dims, at::ScalarType ty) {
+    return t.dim() == dims && t.scalar_type() == ty && (t.size(dims - 1) <= 1 || t.stride(dims - 1) == 1);
+}
+bool same_strides(const at::Tensor &x, const at::Tensor &y) {
+    for (int64_t i = 0; i < x.dim(); ++i)
+        if (x.size(i) > 1 && x.stride(i) != y.stride(i)) return false;
+    return true;
+}
+bool all_fit(const at::Tensor &t) {
+    for (int64_t i = 0; i < t.dim(); ++i)
+        if (!fits(t.size(i))) return false;
+    return true;
+}
+// A paged cache K, V [P, Hkv, page, D] and its table [R, cols]
+bool paged(const at::Tensor &K, const at::Tensor &V, const at::Tensor &tb, int &ld) {
+    return code(K.scalar_type()) >= 0 && rows_of(K, 4, K.scalar_type()) && rows_of(V, 4, K.scalar_type()) &&
+           K.sizes() == V.sizes() && same_strides(K, V) && all_fit(K) && tb.dim() == 2 && table(tb, tb.size(0), ld) &&
+           fits(tb.size(0));
+}
+// k, v [n, Hkv, D] of the cache's type and the same strides
+bool new_rows(const at::Tensor &k, const at::Tensor &v, int64_t n, const at::Tensor &K) {
+    return rows_of(k, 3, K.scalar_type()) && rows_of(v, 3, K.scalar_type()) && k.sizes() == v.sizes() &&
+           same_strides(k, v) && k.size(0) == n && k.size(1) == K.size(1) && k.size(2) == K.size(3) && all_fit(k);
+}
+
+// paged_append(K, V, k, v, table, start, offsets or None)
+PyObject *paged_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    if (n != 7) return declined();
+    Args g{a};
+    const at::Tensor &K = *g.tensor(0), &V = *g.tensor(1), &k = *g.tensor(2), &v = *g.tensor(3), &tb = *g.tensor(4),
+                     &st = *g.tensor(5);
+    const at::Tensor *off = optional(g, 6);
+    int ld = 0;
+    void *s = nullptr;
+    if (!g.ok || !paged(K, V, tb, ld) || k.dim() != 3 || !new_rows(k, v, k.size(0), K) || !ints(st, tb.size(0)) ||
+        (off && !ints(*off, tb.size(0) + 1)) || !stream_of(g, s))
+        return declined();
+    return PyLong_FromLong(fs_paged_append(
+        K.data_ptr(), V.data_ptr(), K.stride(0), K.stride(1), K.stride(2), (int)K.size(0), (int)K.size(2), k.data_ptr(),
+        v.data_ptr(), k.stride(0), k.stride(1), (int)k.size(0), data<int32_t>(&tb), ld, (int)tb.size(1),
+        data<int32_t>(&st), data<int32_t>(off), (int)tb.size(0), (int)K.size(1), (int)K.size(3), code(K.scalar_type()), s));
+}
+
+// paged_attn(q, K, V, table, kv_len, out, workspace, k or None, v or None, scale or None)
+PyObject *paged_attn(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    if (n != 10) return declined();
+    Args g{a};
+    const at::Tensor &q = *g.tensor(0), &K = *g.tensor(1), &V = *g.tensor(2), &tb = *g.tensor(3), &len = *g.tensor(4),
+                     &out = *g.tensor(5), &ws = *g.tensor(6);
+    const at::Tensor *k = optional(g, 7), *v = optional(g, 8);
+    int ld = 0;
+    void *s = nullptr;
+    if (!g.ok || !paged(K, V, tb, ld) || !rows_of(q, 3, K.scalar_type()) || !all_fit(q) || q.size(2) != K.size(3) ||
+        q.size(0) != tb.size(0) || !ints(len, q.size(0)) || !same(out, q) || !out.is_contiguous() ||
+        !ws.is_contiguous() || !k != !v || (k && !new_rows(*k, *v, q.size(0), K)))
+        return declined();
+    double scale = 0;
+    if (a[9] == Py_None) scale = K.size(3) ? std::pow((double)K.size(3), -0.5) : 1.0;
+    else if (PyFloat_CheckExact(a[9])) scale = PyFloat_AS_DOUBLE(a[9]);
+    else return declined();
+    if (!stream_of(g, s)) return declined();
+    return PyLong_FromLong(fs_paged_attn(
+        q.data_ptr(), q.stride(0), q.stride(1), K.data_ptr(), V.data_ptr(), K.stride(0), K.stride(1), K.stride(2),
+        (int)K.size(0), (int)K.size(2), data<int32_t>(&tb), ld, (int)tb.size(1), data<int32_t>(&len), data<void>(k),
+        data<void>(v), k ? k->stride(0) : 0, k ? k->stride(1) : 0, (float)scale, out.data_ptr(), (int)q.size(0),
+        (int)q.size(1), (int)K.size(1), (int)K.size(3), code(K.scalar_type()), ws.data_ptr(), ws.nbytes(), s));
+}
+
+// token_sample(logits, u, temperature, top_k, top_p, min_p (each or None), token, logprob, workspace)
+PyObject *token_sample(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    if (n != 9) return declined();
+    Args g{a};
+    const at::Tensor &lg = *g.tensor(0), &u = *g.tensor(1), &tok = *g.tensor(6), &lp = *g.tensor(7), &ws = *g.tensor(8);
+    const at::Tensor *T = optional(g, 2), *k = optional(g, 3), *p = optional(g, 4), *m = optional(g, 5);
+    void *s = nullptr;
+    if (!g.ok || lg.dim() != 2 || code(lg.scalar_type()) < 0 || !rows_of(lg, 2, lg.scalar_type()) || !all_fit(lg) ||
+        !ws.is_contiguous())
+        return declined();
+    const int64_t R = lg.size(0);
+    auto vec = [&](const at::Tensor *t, at::ScalarType ty) {
+        return !t || (t->dim() == 1 && t->size(0) == R && t->scalar_type() == ty && t->is_contiguous());
+    };
+    if (!vec(&u, at::kFloat) || !vec(T, at::kFloat) || !vec(k, at::kInt) || !vec(p, at::kFloat) || !vec(m, at::kFloat) ||
+        !vec(&tok, at::kInt) || !vec(&lp, at::kFloat) || !stream_of(g, s))
+        return declined();
+    return PyLong_FromLong(fs_token_sample(lg.data_ptr(), R > 1 ? lg.stride(0) : lg.size(1), (int)R, (int)lg.size(1),
+                                           code(lg.scalar_type()), data<float>(&u), data<float>(T), data<int32_t>(k),
+                                           data<float>(p), data<float>(m), data<int32_t>(&tok), data<float>(&lp),
+                                           ws.data_ptr(), ws.nbytes(), s));
+}
+
 // A torch accessor throws for a tensor whose data must not be touched (one made
 // by a tracer, for instance); no exception may cross into the interpreter, so
 // such a call is declined too and the general path raises torch's own error.
@@ -303,6 +400,10 @@ PyMethodDef methods[] = {
     {"beam_select", FS_FAST(select), "(logits, beam_scores, k, c, tokens or None, n, t or -1, scores, beam, token, workspace)"},
     {"cache_reorder", FS_FAST(cache_reorder), "(K, V, parent, k, t or -1)"},
     {"ancestry_step", FS_FAST(ancestry_step), "(anc, parent, k, t)"},
+    {"paged_append", FS_FAST(paged_append), "(K, V, k, v, table, start, offsets or None)"},
+    {"paged_attn", FS_FAST(paged_attn), "(q, K, V, table, kv_len, out, workspace, k or None, v or None, scale or None)"},
+    {"token_sample", FS_FAST(token_sample),
+     "(logits, u, temperature, top_k, top_p, min_p, token, logprob, workspace), settings None: off"},
     {nullptr, nullptr, 0, nullptr},
 };
 

@@ -1,0 +1,362 @@
+"""GPU parity of the paged cache (paged_append, paged_attn) with the fp64 forms.
+
+Cache slots that a call must not read hold NaN, so a read of one shows."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import paged
+from paper_2106_04718_amd import _native as N
+from paper_2106_04718_amd import api, workloads
+
+from _gpu import bits, device, say, to_f64
+
+pytestmark = pytest.mark.gpu
+
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+def draw(rng, shape, dtype, sigma=1.0):
+    x = (rng.standard_normal(shape) * sigma).astype(np.float32)
+    return workloads.f32_to_bf16_bits(x) if dtype == BF16 else x
+
+
+def dev_of(a, dtype=None):
+    a = np.ascontiguousarray(a)
+    if a.dtype == np.uint16:
+        return torch.from_numpy(a.view(np.int16)).to(device()).view(BF16)
+    return torch.from_numpy(a).to(device())
+
+
+def nan_like(shape, dtype):
+    return np.full(shape, workloads.BF16_NAN if dtype == BF16 else np.nan, np.uint16 if dtype == BF16 else np.float32)
+
+
+def make(seed, lens, Hq, Hkv, D, page, dtype, new=False, sigma=1.0, spare=5, extra_cols=0):
+    """A cache whose rows have these lengths, pages in random order, NaN in every
+    slot that no row attends."""
+    rng = np.random.default_rng(seed)
+    lens = np.asarray(lens, np.int32)
+    R = len(lens)
+    need = -(-lens // page)
+    P = int(need.sum()) + spare
+    cols = max(1, int(need.max(initial=0))) + extra_cols
+    ids = rng.permutation(P)
+    table = rng.integers(0, P, (R, cols)).astype(np.int32)   # columns behind a row name pages of others
+    K, V = nan_like((P, Hkv, page, D), dtype), nan_like((P, Hkv, page, D), dtype)
+    at = 0
+    for r in range(R):
+        table[r, :need[r]] = ids[at:at + need[r]]
+        at += need[r]
+        for j in range(need[r]):
+            n = min(page, lens[r] - j * page)
+            K[table[r, j], :, :n] = draw(rng, (Hkv, n, D), dtype, sigma)
+            V[table[r, j], :, :n] = draw(rng, (Hkv, n, D), dtype)
+    d = dict(q=draw(rng, (R, Hq, D), dtype, sigma), K=K, V=V, table=table, kv_len=lens)
+    if new:
+        d.update(k=draw(rng, (R, Hkv, D), dtype, sigma), v=draw(rng, (R, Hkv, D), dtype))
+        for r in range(R):   # the new token's slot is not written yet
+            if lens[r]:
+                pg, sl = table[r, (lens[r] - 1) // page], (lens[r] - 1) % page
+                K[pg, :, sl] = V[pg, :, sl] = nan_like((Hkv, D), dtype)
+    return d
+
+
+def tolerance(d, ref, scale):
+    """Bound of |out - ref|: half a step of the output's type, plus what fp32 can
+    lose: a score of D products and its scaling, exp of it, the sums over the
+    keys (L additions at most, in fp32), weights as two bf16 values (2^-17)."""
+    q, K, V = (paged._f64(d[x]) for x in "qKV")
+    k = np.nan_to_num(K)
+    if "k" in d:
+        k = np.concatenate([k.reshape(-1, k.shape[-1]), paged._f64(d["k"]).reshape(-1, k.shape[-1])])
+    # sum_d |q_d k_d| <= |q| |k|
+    dot = np.sqrt((q ** 2).sum(-1).max(initial=0)) * np.sqrt((k ** 2).sum(-1).max(initial=0)) * abs(scale)
+    D, L = q.shape[-1], int(d["kv_len"].max(initial=0))
+    eps = 2.0 ** -24
+    rel = dot * (D + 8) * eps + 8 * eps + 2.0 ** -17 + (min(L, d["table"].shape[1] * d["K"].shape[2]) + 64) * eps
+    vmax = max(np.abs(np.nan_to_num(V)).max(initial=0), np.abs(paged._f64(d["v"])).max(initial=0) if "v" in d else 0)
+    half = 2.0 ** -8 if d["q"].dtype == np.uint16 else 2.0 ** -24
+    return half * np.abs(ref) + 2 * rel * vmax + 1e-38
+
+
+def run(d, what, scale=None, **kw):
+    say(f"[paged attn] {what}: R={len(d['kv_len'])} q{d['q'].shape} K{d['K'].shape} lens {d['kv_len'].tolist()[:8]}")
+    t = {x: dev_of(d[x]) for x in d}
+    out = api.paged_attn(t["q"], t["K"], t["V"], t["table"], t["kv_len"], k=t.get("k"), v=t.get("v"), scale=scale, **kw)
+    torch.cuda.synchronize()
+    return out, t
+
+
+def check(d, what, scale=None, **kw):
+    out, t = run(d, what, scale, **kw)
+    ref = paged.paged_attn(d["q"], d["K"], d["V"], d["table"], d["kv_len"], d.get("k"), d.get("v"), scale)
+    if "k" in d:
+        ref, K, V = ref
+        assert np.array_equal(bits(t["K"]), K.view(bits(t["K"]).dtype)), f"{what}: K after the write"
+        assert np.array_equal(bits(t["V"]), V.view(bits(t["V"]).dtype)), f"{what}: V after the write"
+    else:
+        assert np.array_equal(bits(t["K"]), d["K"].view(bits(t["K"]).dtype)), f"{what}: K is left as it was"
+    got = to_f64(out)
+    s = d["q"].shape[-1] ** -0.5 if scale is None else scale
+    err, tol = np.abs(got - ref), tolerance(d, ref, s)
+    assert np.isfinite(got).all() and (err <= tol).all(), f"{what}: off by {np.max(err / tol)} of the bound"
+    return out
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("D", [16, 32, 64, 128])
+@pytest.mark.parametrize("Hq,Hkv", [(4, 4), (8, 2), (3, 1)])
+def test_types_widths_and_shared_heads(dtype, D, Hq, Hkv):
+    check(make(D + Hq, [1, 33, 200, 17], Hq, Hkv, D, 16, dtype), "widths")
+    check(make(D + Hq, [64, 1, 130], Hq, Hkv, D, 16, dtype, new=True), "widths, new token")
+
+
+@pytest.mark.parametrize("G", [1, 2, 5, 7, 8, 15, 16, 17, 31, 33, 48])
+def test_query_heads_per_key_value_head(G):
+    check(make(G, [70, 5], 2 * G, 2, 64, 16, BF16, new=True), f"G={G}")
+    check(make(G, [70, 5], G, 1, 32, 8, F32), f"G={G}")
+
+
+@pytest.mark.parametrize("page", [1, 2, 3, 5, 7, 16, 24, 100, 128, 257])
+def test_page_sizes(page):
+    check(make(page, [1, 31, 32, 33, 150, 300], 4, 2, 64, page, BF16, new=page % 2 == 1), f"page={page}")
+    check(make(page, [1, 2, 40, 259], 2, 2, 32, page, F32, new=page % 2 == 0), f"page={page}")
+
+
+@pytest.mark.parametrize("new", [False, True])
+def test_every_length_around_the_tiles(new):
+    lens = list(range(0, 70)) + [95, 96, 97, 127, 128, 129, 255, 256, 257, 511, 512, 513, 1025]
+    check(make(7, lens, 4, 1, 64, 16, BF16, new=new), "lengths")
+    check(make(8, lens, 2, 2, 16, 8, F32, new=new), "lengths")
+
+
+@pytest.mark.parametrize("dtype,lens", [(BF16, [9000]), (BF16, [1, 20000, 0, 3]), (F32, [5000, 2]), (BF16, [4097] * 3)])
+def test_few_long_rows(dtype, lens):
+    check(make(len(lens), lens, 8, 2, 64, 64, dtype, new=True, sigma=0.5), "long rows")
+
+
+def test_many_short_rows_and_one_long():
+    rng = np.random.default_rng(5)
+    lens = rng.integers(0, 40, 700)
+    lens[345] = 6000
+    check(make(9, lens, 4, 2, 64, 16, BF16, new=True), "one long row")
+    check(make(10, np.ones(2000, int), 2, 1, 16, 16, BF16, new=True), "2000 rows of one position")
+
+
+def test_rows_of_nothing():
+    d = make(11, [0, 5, 0, 0], 4, 2, 64, 16, BF16, new=True)
+    out = check(d, "empty rows")
+    assert not to_f64(out)[[0, 2, 3]].any()
+    d = make(12, [0, 0], 4, 2, 64, 16, F32)
+    assert not to_f64(check(d, "only empty rows")).any()
+
+
+def test_bad_pages_lengths_and_scores():
+    d = make(13, [100, 90, 64, 300], 4, 2, 64, 16, BF16, extra_cols=1)
+    d["table"][0, 2] = -1                      # one page in the middle
+    d["table"][1, :] = [d["K"].shape[0], -7, 2**31 - 1, -2**31] * 5   # every page
+    d["table"][2, 3] = d["K"].shape[0]         # the last page
+    d["kv_len"][3] = 2**31 - 1                 # past the table: clamped, and the last column names a page
+    P = d["K"].shape[0]
+    d["table"][3, -2:] = P                     # of none
+    d["kv_len"] = np.append(d["kv_len"], [-5]).astype(np.int32)
+    d["table"] = np.concatenate([d["table"], d["table"][:1]])
+    d["q"] = np.concatenate([d["q"], d["q"][:1]])
+    # NaN where L of row 3 was 300: its page's remaining slots are attended now
+    d["K"], d["V"] = (np.where(x == workloads.BF16_NAN, np.uint16(0), x) for x in (d["K"], d["V"]))
+    out = to_f64(check(d, "bad pages"))
+    assert not out[1].any() and not out[4].any()
+
+
+def test_new_token_without_a_page_writes_nothing():
+    d = make(14, [33, 33, 0], 4, 2, 64, 16, BF16, new=True)
+    d["table"][0, 2] = -1
+    d["kv_len"] = np.array([33, 33, 0], np.int32)
+    check(d, "no page for the new token")
+
+
+def test_large_scores_and_one_key_that_takes_all():
+    d = make(15, [400, 77], 4, 2, 64, 16, F32, sigma=20.0)
+    check(d, "scores of hundreds")
+    check(make(16, [400, 77], 4, 2, 64, 16, BF16), "scale 0", scale=0.0)
+    check(make(17, [400, 77], 4, 2, 64, 16, BF16), "negative scale", scale=-0.3)
+    d = make(18, [300], 1, 1, 64, 16, F32)
+    d["q"][:] = 1e4
+    d["K"][:] = np.where(np.isnan(d["K"]), np.nan, -1e4).astype(np.float32)   # every score -6.4e9 / 8
+    check(d, "all scores equal and very low")
+
+
+def test_infinite_values_stay_where_they_are_attended():
+    d = make(19, [40, 40], 2, 1, 16, 16, F32)
+    d["V"][d["table"][0, 1], 0, 3, 5] = np.inf
+    out, _ = run(d, "an infinite value")
+    got = to_f64(out)
+    assert np.isposinf(got[0, :, 5]).all() and np.isfinite(np.delete(got[0], 5, 1)).all() and np.isfinite(got[1]).all()
+    d["K"][d["table"][1, 0], 0, 0, 0] = np.nan   # a NaN key poisons its row alone
+    out, _ = run(d, "a NaN key")
+    assert np.isnan(to_f64(out)[1]).all() and not np.isnan(to_f64(out)[0]).any()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_strides(dtype):
+    """Token-major pages, keys and values interleaved, q, k and v cut from one
+    projection, a table with a leading dimension: the same bits."""
+    R, Hq, Hkv, D, page = 3, 4, 2, 64, 16
+    d = make(20, [50, 1, 130], Hq, Hkv, D, page, dtype, new=True)
+    want, t0 = run(d, "contiguous")
+    dev = device()
+    P = d["K"].shape[0]
+    kv = torch.empty(P, page, 2, Hkv, D, dtype=dtype, device=dev)
+    K, V = kv[:, :, 0].transpose(1, 2), kv[:, :, 1].transpose(1, 2)
+    K.copy_(dev_of(d["K"])), V.copy_(dev_of(d["V"]))
+    qkv = torch.empty(R, Hq + 2 * Hkv, D, dtype=dtype, device=dev)
+    q, k, v = qkv.split([Hq, Hkv, Hkv], 1)
+    q.copy_(dev_of(d["q"])), k.copy_(dev_of(d["k"])), v.copy_(dev_of(d["v"]))
+    table = torch.full((R, 40), -1, dtype=torch.int32, device=dev)
+    table[:, :d["table"].shape[1]] = dev_of(d["table"])
+    table = table[:, :d["table"].shape[1]]
+    out = api.paged_attn(q, K, V, table, dev_of(d["kv_len"]), k=k, v=v)
+    torch.cuda.synchronize()
+    assert np.array_equal(bits(out), bits(want))
+    assert np.array_equal(bits(K.contiguous()), bits(t0["K"])) and np.array_equal(bits(V.contiguous()), bits(t0["V"]))
+
+
+def test_the_same_call_twice_gives_the_same_bits_and_any_workspace_serves():
+    big = make(21, [9000, 40, 700], 8, 2, 128, 16, BF16)
+    small = make(22, [300, 2], 4, 4, 32, 8, F32)
+    ws = api.new_workspace(max(api.paged_attn_workspace_bytes(3, 8, 2, 16, big["table"].shape[1], 128),
+                               api.paged_attn_workspace_bytes(2, 4, 4, 8, small["table"].shape[1], 32, F32)), device())
+    first = [bits(run(x, "fresh workspace")[0]) for x in (big, small)]
+    for _ in range(3):   # sizes that alternate in one workspace
+        for x, want in zip((big, small), first):
+            assert np.array_equal(bits(run(x, "shared workspace", workspace=ws)[0]), want)
+
+
+def test_a_row_does_not_depend_on_its_neighbours():
+    """Alone and in a batch a row differs in nothing but the split over its length:
+    both within the bound."""
+    d = make(23, [1500, 3, 800, 0, 64], 8, 2, 64, 16, BF16)
+    whole = to_f64(check(d, "batch"))
+    for r in range(5):
+        one = dict(d, q=d["q"][r:r + 1], table=d["table"][r:r + 1], kv_len=d["kv_len"][r:r + 1])
+        assert (np.abs(to_f64(check(one, f"row {r} alone")) - whole[r]) <= 2.0 ** -7 * np.abs(whole[r]) + 1e-4).all()
+
+
+def test_cache_behind_32_bits():
+    """A page table that reaches past 4 GiB of a cache."""
+    dev = device()
+    P, Hkv, page, D = 70_000, 4, 128, 128          # 9.2 GB in bf16
+    K = torch.empty(P, Hkv, page, D, dtype=BF16, device=dev)
+    V = torch.empty_like(K)
+    rng = np.random.default_rng(24)
+    d = make(24, [300, 129], 8, Hkv, D, page, BF16, new=True)
+    far = np.array([P - 1, 0, 40_000, 33_000, 65_535, 16_384, 32_768, 8192, 1, 2], np.int32)[:d["K"].shape[0]]
+    K[torch.from_numpy(far).long().to(dev)] = dev_of(d["K"])
+    V[torch.from_numpy(far).long().to(dev)] = dev_of(d["V"])
+    want, t0 = run(d, "near pages")
+    out = api.paged_attn(dev_of(d["q"]), K, V, dev_of(far[d["table"]]), dev_of(d["kv_len"]), k=dev_of(d["k"]), v=dev_of(d["v"]))
+    torch.cuda.synchronize()
+    assert np.array_equal(bits(out), bits(want))
+    assert np.array_equal(bits(K[torch.from_numpy(far).long().to(dev)]), bits(t0["K"]))
+
+
+# ---- paged_append ------------------------------------------------------------------
+
+def append_case(seed, lens, used, Hkv, D, page, dtype, lead=0, trail=0):
+    rng = np.random.default_rng(seed)
+    lens, used = np.asarray(lens), np.asarray(used)
+    need = -(-(lens + used) // page)
+    P = int(need.sum()) + 3
+    ids, at = rng.permutation(P), 0
+    table = np.full((len(lens), max(1, int(need.max(initial=0)))), -1, np.int32)
+    for r, n in enumerate(need):
+        table[r, :n] = ids[at:at + n]
+        at += n
+    N_ = lead + int(lens.sum()) + trail
+    off = (lead + np.concatenate([[0], np.cumsum(lens)])).astype(np.int32)
+    return dict(K=draw(rng, (P, Hkv, page, D), dtype), V=draw(rng, (P, Hkv, page, D), dtype),
+                k=draw(rng, (N_, Hkv, D), dtype), v=draw(rng, (N_, Hkv, D), dtype), table=table,
+                start=used.astype(np.int32), offsets=off)
+
+
+def check_append(d, what, with_offsets=True):
+    say(f"[paged append] {what}: K{d['K'].shape} k{d['k'].shape} {d['K'].dtype}")
+    t = {x: dev_of(d[x]) for x in d}
+    api.paged_append(t["K"], t["V"], t["k"], t["v"], t["table"], t["start"], t["offsets"] if with_offsets else None)
+    torch.cuda.synchronize()
+    K, V = paged.paged_append(d["K"], d["V"], d["k"], d["v"], d["table"], d["start"], d["offsets"] if with_offsets else None)
+    assert np.array_equal(bits(t["K"]), K.view(bits(t["K"]).dtype)), f"{what}: K"
+    assert np.array_equal(bits(t["V"]), V.view(bits(t["V"]).dtype)), f"{what}: V"
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("D", [16, 32, 64, 128])
+@pytest.mark.parametrize("Hkv,page", [(1, 1), (3, 7), (8, 16)])
+def test_append_types_and_sizes(dtype, D, Hkv, page):
+    check_append(append_case(D, [5, 0, 1, 40], [3, 9, 0, 30], Hkv, D, page, dtype), "ragged")
+    check_append(append_case(D, [5, 0, 1, 40], [3, 9, 0, 30], Hkv, D, page, dtype, lead=2, trail=6), "padded")
+    check_append(append_case(D, [1] * 9, list(range(9)), Hkv, D, page, dtype), "one per row", with_offsets=False)
+
+
+def test_append_many_rows_and_long_prompts():
+    rng = np.random.default_rng(30)
+    check_append(append_case(31, rng.integers(0, 3, 1500), rng.integers(0, 50, 1500), 2, 16, 16, BF16), "1500 rows")
+    check_append(append_case(32, [3000, 1, 1999], [0, 5, 17], 4, 64, 16, BF16), "long prompts")
+    check_append(append_case(33, np.zeros(7, int), np.zeros(7, int), 2, 16, 16, BF16, trail=5), "nobody's tokens")
+
+
+def test_append_skips_what_has_no_slot():
+    d = append_case(34, [6, 6, 6, 6], [0, 0, 0, 0], 2, 32, 4, BF16)
+    d["table"][0, 1] = -1
+    d["table"][1, 0] = d["K"].shape[0]
+    d["start"][2], d["start"][3] = -3, 2**31 - 3
+    check_append(d, "no slot")
+
+
+def test_append_strided_and_far():
+    dev = device()
+    d = append_case(35, [9, 4], [2, 0], 2, 64, 16, BF16)
+    P = d["K"].shape[0]
+    kv = torch.zeros(P, 16, 2, 2, 64, dtype=BF16, device=dev)
+    K, V = kv[:, :, 0].transpose(1, 2), kv[:, :, 1].transpose(1, 2)
+    K.copy_(dev_of(d["K"])), V.copy_(dev_of(d["V"]))
+    both = torch.empty(13, 6, 64, dtype=BF16, device=dev)
+    k, v = both[:, 1:3], both[:, 4:6]
+    k.copy_(dev_of(d["k"])), v.copy_(dev_of(d["v"]))
+    api.paged_append(K, V, k, v, dev_of(d["table"]), dev_of(d["start"]), dev_of(d["offsets"]))
+    torch.cuda.synchronize()
+    wK, wV = paged.paged_append(d["K"], d["V"], d["k"], d["v"], d["table"], d["start"], d["offsets"])
+    assert np.array_equal(bits(K.contiguous()), wK) and np.array_equal(bits(V.contiguous()), wV)
+
+
+def test_empty_calls():
+    dev = device()
+    K = torch.zeros(2, 2, 16, 64, dtype=BF16, device=dev)
+    e = lambda *s, t=BF16: torch.empty(*s, dtype=t, device=dev)
+    api.paged_append(K, K.clone(), e(0, 2, 64), e(0, 2, 64), e(3, 1, t=torch.int32), e(3, t=torch.int32),
+                     torch.zeros(4, dtype=torch.int32, device=dev))
+    assert api.paged_attn(e(0, 4, 64), K, K.clone(), e(0, 1, t=torch.int32), e(0, t=torch.int32)).shape == (0, 4, 64)
+    out = api.paged_attn(e(2, 4, 64), K, K.clone(), e(2, 0, t=torch.int32), torch.full((2,), 9, dtype=torch.int32, device=dev))
+    assert not out.any()   # a table without columns
+
+
+@pytest.mark.parametrize("change,needle", [
+    (dict(q=lambda x: x["q"].float()), "q must be"), (dict(q=lambda x: x["q"][0]), "dimensions"),
+    (dict(K=lambda x: x["K"].transpose(2, 3).contiguous().transpose(2, 3)), "contiguous rows"),
+    (dict(V=lambda x: x["V"].transpose(0, 1).contiguous().transpose(0, 1)), "same shape and strides"),
+    (dict(table=lambda x: x["table"].long()), "table must be"), (dict(kv_len=lambda x: x["kv_len"][:1]), "kv_len must be"),
+    (dict(kv_len=lambda x: x["kv_len"].cpu()), "GPU tensor"), (dict(k=lambda x: x["q"][:, :2].clone()), "go together"),
+    (dict(out=lambda x: x["q"]), "overlaps"), (dict(out=lambda x: x["q"].float()), "out must match"),
+    (dict(workspace=lambda x: torch.zeros(8, dtype=torch.uint8, device=x["q"].device)), "workspace of 8 bytes"),
+    (dict(q=lambda x: x["q"][:, :3].contiguous()), "multiple of Hkv"), (dict(scale=lambda x: math.inf), "scale"),
+    (dict(table=lambda x: x["table"][:1]), "shape mismatch"),
+])
+def test_refusals_of_the_front_end(change, needle):
+    d = make(40, [20, 5], 4, 2, 64, 16, BF16)
+    x = {n: dev_of(a) for n, a in d.items()}
+    x.update({n: f(x) for n, f in change.items()})
+    with pytest.raises((ValueError, N.NativeError), match=needle):
+        api.paged_attn(x.pop("q"), x.pop("K"), x.pop("V"), x.pop("table"), x.pop("kv_len"), **x)
