@@ -535,7 +535,7 @@ void fs_postproc_destroy(fs_postproc *pp);
  *   stream       hipStream_t (NULL = default stream)
  * Supported: dtype FS_F32 or FS_BF16, D in {16, 32, 64, 128}, any page >= 1,
  * pointers of K, V, k, v and the strides multiples of 16 bytes, K and V of at
- * most 64 GiB each, cols * page below 2^31.  Byte copies: exact.
+ * most 64 GiB each, cols * page at most 2^30.  Byte copies: exact.
  * Errors: FS_ERR_INVALID_ARG for negative sizes or strides, page < 1, ld_table
  * < cols, P < 1, N != R without offsets, null or misaligned pointers, or the
  * cache overlapping an input (K and V may be interleaved in one allocation);

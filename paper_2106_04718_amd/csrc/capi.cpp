@@ -717,8 +717,8 @@ int check_paged(const void *K, const void *V, int64_t page_stride, int64_t head_
         return fail(FS_ERR_INVALID_ARG, "the cache's strides must be multiples of 16 bytes");
     const long long e = extent(P, page_stride, Hkv, head_stride, page, slot_stride, D, esize);
     if (e < 0 || e > (64ll << 30)) return fail(FS_ERR_UNSUPPORTED, "K and V may span at most 64 GiB each");
-    if ((long long)cols * page > INT_MAX)
-        return fail(FS_ERR_UNSUPPORTED, "a table of %d pages of %d positions exceeds 2^31 positions", cols, page);
+    if ((long long)cols * page > (1 << 30))
+        return fail(FS_ERR_UNSUPPORTED, "a table of %d pages of %d positions exceeds 2^30 positions", cols, page);
     *kv_bytes = (size_t)e;
     *table_bytes = cols > 0 ? ((size_t)(R - 1) * ld_table + cols) * 4 : 0;
     return FS_OK;
@@ -742,8 +742,8 @@ int check_paged_attn_sizes(int R, int Hq, int Hkv, int page, int cols, int D, in
     if (Hkv == 0 ? Hq != 0 : Hq % Hkv != 0)
         return fail(FS_ERR_INVALID_ARG, "Hq=%d is not a multiple of Hkv=%d", Hq, Hkv);
     if ((long long)R * Hq > (1 << 24)) return fail(FS_ERR_UNSUPPORTED, "R*Hq=%lld exceeds 2^24", (long long)R * Hq);
-    if ((long long)cols * page > INT_MAX)
-        return fail(FS_ERR_UNSUPPORTED, "a table of %d pages of %d positions exceeds 2^31 positions", cols, page);
+    if ((long long)cols * page > (1 << 30))
+        return fail(FS_ERR_UNSUPPORTED, "a table of %d pages of %d positions exceeds 2^30 positions", cols, page);
     return FS_OK;
 }
 
