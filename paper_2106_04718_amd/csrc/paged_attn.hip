@@ -47,6 +47,7 @@ constexpr int kUnit = kTile * kWaves;   // positions a workgroup attends at a ti
 constexpr int kHeads = 16;              // query heads of a workgroup
 constexpr int kTaskBits = 10;
 constexpr int kTasks = 1 << kTaskBits;  // chunks aimed at: four for each of the 256 CUs
+constexpr int kJoin = 64;               // states joined at a time
 constexpr int kScanRows = 256;          // rows whose lengths every workgroup looks at: four a lane
 
 typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
@@ -97,10 +98,9 @@ __device__ __forceinline__ bool find_task(const PagedAttn &a, int ht, int t, Tas
     const int lane = (int)threadIdx.x & 63;
     int u[4], s[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int r = 4 * lane + i;
-        u[i] = r < a.R ? units_of(clamp_len(a, a.kv_len[r])) : 0;
-    }
+    for (int i = 0; i < 4; ++i) u[i] = a.kv_len[4 * lane + i < a.R ? 4 * lane + i : a.R - 1];   // all in flight at once
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u[i] = 4 * lane + i < a.R ? units_of(clamp_len(a, u[i])) : 0;
     // the sum may pass 32 bits: the upper and lower halves of the units apart
     int lo = 0, hi = 0;
 #pragma unroll
@@ -219,9 +219,9 @@ struct Tile {
     }
     // row: the lane's key row
     __device__ __forceinline__ void load_k(int kb, const unsigned char *row, int g) {
-        if constexpr (BF16 && D == 16) {
-            k[kb][0] = u32x4_t{0u, 0u, 0u, 0u};
-            if (g < 2) k[kb][0] = load16(row + 16 * g);
+        if constexpr (BF16 && D == 16) {   // the upper half meets zeros of the queries: it has to be finite
+            k[kb][0] = load16(row + 16 * (g & 1));
+            if (g >= 2) k[kb][0] = u32x4_t{0u, 0u, 0u, 0u};
         } else {
 #pragma unroll
             for (int s = 0; s < kSteps; ++s) k[kb][s] = load16(row + 64 * s + 16 * g);
@@ -286,6 +286,17 @@ struct Tile {
     }
 };
 
+// The states of cut rows go past the caches, which the chip's eight L2s do not
+// keep coherent for ordinary accesses: these are, one by one.  (Ordinary ones
+// between release and acquire fences write back and invalidate a whole L2 per
+// chunk: 64 ragged rows of some 2000 positions took 314 us in place of 115.)
+__device__ __forceinline__ void put(float *p, float x) {
+    __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float get(const float *p) {
+    return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
 // exp2 of m - top, where m == -inf has no weight whatever top is.
 __device__ __forceinline__ float weight(float m, float top) {
     return __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.f : top));
@@ -297,21 +308,19 @@ __device__ __forceinline__ void store_out(unsigned char *out, size_t i, float x)
     else reinterpret_cast<float *>(out)[i] = x;
 }
 
-// Joins n states of one head, stride floats apart: element d of the output, the
-// maximum and the sum (negative: no position at all).
+// Joins the waves' states of one head: element d of the output, the maximum and
+// the sum (negative: no position at all).
 template <typename Load>
-__device__ __forceinline__ void join(int n, Load load, float &o, float &m, float &l) {
-    float top = -INFINITY;
-    for (int i = 0; i < n; ++i) top = fmaxf(top, load(i, 1));
+__device__ __forceinline__ void join(Load load, float &o, float &m, float &l) {
+    m = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) m = fmaxf(m, load(i, 1));
     o = 0.f, l = -1.f;
-    for (int i = 0; i < n; ++i) {
-        const float li = load(i, 2);
-        if (li < 0.f) continue;
-        const float w = weight(load(i, 1), top);
-        l = (l < 0.f ? 0.f : l) + li * w;
-        o += load(i, 0) * w;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) {
+        const float li = load(i, 2), w = weight(load(i, 1), m);
+        if (!(li < 0.f)) l = (l < 0.f ? 0.f : l) + li * w, o += load(i, 0) * w;
     }
-    m = top;
 }
 
 template <int D, bool BF16>
@@ -319,8 +328,10 @@ __global__ __launch_bounds__(kBlock, 2) void paged_attn_kernel(PagedAttn a, Geo 
 {
     using T = Tile<D, BF16>;
     constexpr int kEsize = BF16 ? 2 : 4, kPad = D + 4;
+    constexpr bool kHalf = BF16 && D == 16;   // a row is half of what an instruction contracts
     __shared__ __align__(16) float so[kWaves][kHeads][kPad];
     __shared__ float sm[kWaves][kHeads], sl[kWaves][kHeads];
+    __shared__ float sf[kJoin][kHeads], sg[kJoin][kHeads];
     __shared__ unsigned arrived;
 
     const int lane = (int)threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
@@ -347,10 +358,10 @@ __global__ __launch_bounds__(kBlock, 2) void paged_attn_kernel(PagedAttn a, Geo 
         const unsigned char *qp = a.q + (size_t)r * a.q_row_bytes +
                                   (size_t)(h * geo.G + qt * kHeads + (n < heads ? n : 0)) * a.q_head_bytes;
 #pragma unroll
+        for (int s = 0; s < T::kSteps; ++s) q[s] = *reinterpret_cast<const u32x4_t *>(qp + 64 * s + 16 * (kHalf ? g & 1 : g));
+#pragma unroll
         for (int s = 0; s < T::kSteps; ++s) {
-            q[s] = u32x4_t{0u, 0u, 0u, 0u};
-            if (n < heads && (!(BF16 && D == 16) || g < 2))
-                q[s] = *reinterpret_cast<const u32x4_t *>(qp + 64 * s + 16 * g);
+            if (n >= heads || (kHalf && g >= 2)) q[s] = u32x4_t{0u, 0u, 0u, 0u};
         }
     }
     const PagedCache &c = a.cache;
@@ -364,7 +375,8 @@ __global__ __launch_bounds__(kBlock, 2) void paged_attn_kernel(PagedAttn a, Geo 
     // tile's positions that exist.
     auto page_of = [&](int t0) {
         const int pos = t0 + (lane & 31);
-        return pos < end ? table[geo.by_page((unsigned)pos)] : -1;
+        const int pg = table[geo.by_page((unsigned)(pos < end ? pos : begin))];
+        return pos < end ? pg : -1;
     };
     auto slot_of = [&](int t0, int pg, unsigned &off, unsigned &live) {
         const int pos = t0 + (lane & 31);
@@ -394,37 +406,25 @@ __global__ __launch_bounds__(kBlock, 2) void paged_attn_kernel(PagedAttn a, Geo 
     float m = -INFINITY, l = 0.f;
     bool any = false;
 
-    int t0 = begin + w * kTile;
-    unsigned off = 0, live = 0;
-    int pg = t0 < end ? page_of(t0) : -1, pg_next = -1;
-    if (t0 < end) {
-        if (end - t0 > kUnit) pg_next = page_of(t0 + kUnit);
-        slot_of(t0, pg, off, live);
-        load_k(t0, off);
-        load_v(t0, off);
-    }
-    while (t0 < end) {
-        f32x4_t sc[2];
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) sc[kb] = x.scores(kb, q);
-        const bool more = end - t0 > kUnit;
-        const int t1 = more ? t0 + kUnit : t0;
-        unsigned off_next = 0, live_next = 0;
-        if (more) {
-            slot_of(t1, pg_next, off_next, live_next);
-            pg_next = end - t1 > kUnit ? page_of(t1 + kUnit) : -1;
-            load_k(t1, off_next);
-        }
+    // the softmax of a tile's scores, then its values
+    auto attend = [&](f32x4_t (&sc)[2], unsigned live) {
         float mx = -INFINITY;
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                sc[kb][i] *= scale;
-                if (live != 0xffffffffu && !((live >> (16 * kb + 4 * g + i)) & 1u)) sc[kb][i] = -INFINITY;
-                mx = fmaxf(mx, sc[kb][i]);
+            for (int i = 0; i < 4; ++i) sc[kb][i] *= scale;
+        }
+        if (live != 0xffffffffu) {   // a position that is not there read anything: its weight is 0, its value too
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const bool is = (live >> (16 * (j / 4) + 4 * g + j % 4)) & 1u;
+                sc[j / 4][j % 4] = is ? sc[j / 4][j % 4] : -INFINITY;
+#pragma unroll
+                for (int e = 0; e < T::kVwords; ++e) x.v[j][e] = is ? x.v[j][e] : 0u;
             }
         }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) mx = fmaxf(mx, sc[j / 4][j % 4]);
         any |= live != 0u;
         mx = fmaxf(m, col_max(mx));
         if (__any(mx > m)) {
@@ -440,16 +440,37 @@ __global__ __launch_bounds__(kBlock, 2) void paged_attn_kernel(PagedAttn a, Geo 
             p[j] = weight(sc[j / 4][j % 4], m);
             l += p[j];
         }
-        if (live != 0xffffffffu) {   // a position that is not there may read anything: its weight is 0, its value too
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const bool is = (live >> (16 * (j / 4) + 4 * g + j % 4)) & 1u;
-#pragma unroll
-                for (int e = 0; e < T::kVwords; ++e) x.v[j][e] = is ? x.v[j][e] : 0u;
-            }
-        }
         x.accumulate(p, o);
-        if (fresh >= t0 && fresh - t0 < kTile && qt == 0 && ((live >> (fresh - t0)) & 1u)) {   // the new token's own row
+    };
+
+    int t0 = begin + w * kTile;
+    if (t0 < end) {
+        // The keys of the next tile are asked for as soon as this tile's scores
+        // are there, its values behind this tile's: a tile of each is always on
+        // its way.  Loads stand outside of every branch, or the compiler waits
+        // for all of them where the branches meet.
+        unsigned off, live;
+        f32x4_t sc[2];
+        const int pg = page_of(t0);
+        int pg_next = page_of(end - t0 > kUnit ? t0 + kUnit : t0);
+        slot_of(t0, pg, off, live);
+        load_k(t0, off);
+        load_v(t0, off);
+        while (end - t0 > kUnit) {
+            const int t1 = t0 + kUnit;
+            sc[0] = x.scores(0, q), sc[1] = x.scores(1, q);
+            unsigned off_next, live_next;
+            slot_of(t1, pg_next, off_next, live_next);
+            pg_next = page_of(end - t1 > kUnit ? t1 + kUnit : t1);
+            load_k(t1, off_next);
+            attend(sc, live);
+            load_v(t1, off_next);
+            t0 = t1, off = off_next, live = live_next;
+        }
+        sc[0] = x.scores(0, q), sc[1] = x.scores(1, q);
+        attend(sc, live);
+        // the new token's own row: it is in the last tile of the wave that has it
+        if (fresh >= t0 && fresh - t0 < kTile && qt == 0 && ((live >> (fresh - t0)) & 1u)) {
             const size_t to = (size_t)(unsigned)__builtin_amdgcn_readlane((int)off, fresh - t0) * 16;
             constexpr int kPer = D * kEsize / 16;
             if (lane < kPer) {
@@ -459,9 +480,6 @@ __global__ __launch_bounds__(kBlock, 2) void paged_attn_kernel(PagedAttn a, Geo 
                     *reinterpret_cast<const u32x4_t *>(a.v + fresh_off + 16 * lane);
             }
         }
-        if (more) load_v(t1, off_next);
-        off = off_next, live = live_next;
-        t0 = more ? t1 : end;
     }
 
     // the four waves' states, joined
@@ -481,23 +499,24 @@ __global__ __launch_bounds__(kBlock, 2) void paged_attn_kernel(PagedAttn a, Geo 
     for (int i = (int)threadIdx.x; i < heads * D; i += kBlock) {
         const int hd = i / D, d = i % D;
         float oo, mm, ll;
-        join(kWaves, [&](int k, int what) { return what == 0 ? so[k][hd][d] : what == 1 ? sm[k][hd] : sl[k][hd]; }, oo, mm, ll);
+        join([&](int k, int what) { return what == 0 ? so[k][hd][d] : what == 1 ? sm[k][hd] : sl[k][hd]; }, oo, mm, ll);
         if (whole) {
             store_out<BF16>(out, i, ll < 0.f ? 0.f : oo / ll);
         } else {
-            rec[i] = oo;
-            if (d == 0) rec[geo.heads * D + 2 * hd] = mm, rec[geo.heads * D + 2 * hd + 1] = ll;
+            put(rec + i, oo);
+            if (d == 0) put(rec + geo.heads * D + 2 * hd, mm), put(rec + geo.heads * D + 2 * hd + 1, ll);
         }
     }
     if (whole) return;
 
-    // Arrivals.  A record is written before its workgroup counts itself (release),
-    // and read by the workgroup that counts last (acquire); counters end at zero.
-    int group = task.splits;   // chunks of a group
+    // Arrivals.  A record has arrived before its workgroup counts itself, and is
+    // read by the workgroup that counts last; counters end at zero.
+    int group = task.splits;   // chunks of a group: at most 64, and as many groups (a row has at most kTasks + 1)
     if (task.splits > 16) {
         group = 16;
         while (group * group < task.splits) group *= 2;
     }
+    static_assert((kJoin & (kJoin - 1)) == 0 && kJoin * kJoin >= kTasks + 1, "groups and their number fit the arrays");
     const int groups = (task.splits + group - 1) / group;
     for (int level = 0; level < 2; ++level) {
         // level 0: the chunks of this one's group, into its first record; level 1: the groups
@@ -506,34 +525,54 @@ __global__ __launch_bounds__(kBlock, 2) void paged_attn_kernel(PagedAttn a, Geo 
         const int count = level == 0 ? (task.splits - first < group ? task.splits - first : group) : groups;
         const int step = level == 0 ? 1 : group;
         unsigned *counter = (level == 0 ? geo.group_count : geo.row_count) + (size_t)(task.slot + first) * geo.ht + ht;
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "agent");
+        __builtin_amdgcn_s_waitcnt(0);   // this thread's stores have arrived, then everybody's
         __syncthreads();
         if (threadIdx.x == 0)
             arrived = count > 1 ? __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0u;
         __syncthreads();
         if (arrived != (unsigned)count - 1) return;
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
         if (threadIdx.x == 0 && count > 1) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         float *base = geo.records + ((size_t)(task.slot + first) * geo.ht + ht) * geo.record;
         const size_t stride = (size_t)step * geo.ht * geo.record;
         const bool last = level == 1 || groups == 1;
-        for (int i0 = 0; i0 < heads * D; i0 += kBlock) {
-            const int i = i0 + (int)threadIdx.x;
-            const int hd = i / D, d = i % D;
-            float oo = 0.f, mm = 0.f, ll = 0.f;
-            if (i < heads * D)
-                join(count, [&](int k, int what) {
-                    return base[k * stride + (what == 0 ? i : geo.heads * D + 2 * hd + what - 1)];
-                }, oo, mm, ll);
-            if (last) {
-                if (i < heads * D) store_out<BF16>(out, i, ll < 0.f ? 0.f : oo / ll);
-            } else {
-                __syncthreads();   // D divides kBlock or is divided by it: a head's states are all read here
-                if (i < heads * D) {
-                    base[i] = oo;
-                    if (d == 0) base[geo.heads * D + 2 * hd] = mm, base[geo.heads * D + 2 * hd + 1] = ll;
-                }
+        // each state's share of the joined one: exp2 of its maximum's distance, in sf
+        for (int i = (int)threadIdx.x; i < count * heads; i += kBlock) {
+            const int k = i / heads, hd = i - k * heads;
+            const float *state = base + k * stride + geo.heads * D + 2 * hd;
+            const float mm = get(state), ll = get(state + 1);
+            sf[k][hd] = ll < 0.f ? -INFINITY : mm, sg[k][hd] = ll;
+        }
+        __syncthreads();
+        if ((int)threadIdx.x < heads) {
+            const int hd = (int)threadIdx.x;
+            float top = -INFINITY, sum = -1.f;
+            for (int k = 0; k < count; ++k) top = fmaxf(top, sf[k][hd]);
+            for (int k = 0; k < count; ++k) {
+                const float f = weight(sf[k][hd], top), ll = sg[k][hd];
+                sf[k][hd] = f;
+                if (!(ll < 0.f)) sum = (sum < 0.f ? 0.f : sum) + ll * f;
             }
+            sm[0][hd] = top, sl[0][hd] = sum;
+        }
+        __syncthreads();
+        for (int i = (int)threadIdx.x; i < heads * D; i += kBlock) {
+            const int hd = i / D;
+            float oo = 0.f;
+            for (int k0 = 0; k0 < count; k0 += 8) {   // eight on their way at a time
+                float x[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) x[k] = get(base + (k0 + k < count ? k0 + k : k0) * stride + i);
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (k0 + k < count) oo += x[k] * sf[k0 + k][hd];
+            }
+            const float ll = sl[0][hd];
+            if (last) store_out<BF16>(out, i, ll < 0.f ? 0.f : oo / ll);
+            else put(base + i, oo);   // read by this thread alone
+        }
+        if (!last && (int)threadIdx.x < heads) {
+            const int hd = (int)threadIdx.x;
+            put(base + geo.heads * D + 2 * hd, sm[0][hd]), put(base + geo.heads * D + 2 * hd + 1, sl[0][hd]);
         }
     }
 }
