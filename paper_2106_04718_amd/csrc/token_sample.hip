@@ -12,7 +12,20 @@
 // of the kept w exceeds u times their total.
 //
 // A draw next to a border of two tokens depends on the sums, and a large
-// vocabulary has many borders: the weights and sums are 64-bit.
+// vocabulary has many borders: with the weights in 32 bits one draw in some ten
+// thousand would be another token's.  Weights and sums are 64-bit.
+//
+// One workgroup has a row, in registers up to 65536 logits (more are read again
+// by each pass).  No pass sorts or scans the row:
+//   top-k      The k-th largest of the threads' 1024 maxima is a bound that at
+//              least k logits reach, and few more do.  Those go to a list in LDS,
+//              which is sorted; top-p, min-p and the draw happen in the list.
+//   top-p      alone: one pass adds up all weights, and those that can matter
+//              (together the others have less than half of 1 - p) by value, in
+//              2048 bins.  The list is the bin in which the mass reaches p.
+//   otherwise  (no cut, or the list's capacity exceeded, or k above kTopK) the cut
+//              is found by digits of the logits' bits, and the draw by the waves'
+//              sums and the part of the row of the wave that holds it.
 #include <math.h>
 #include <stdint.h>
 
@@ -24,13 +37,17 @@ namespace {
 constexpr int kWave = 64;
 constexpr int kWaves = 16;
 constexpr int kBlock = kWave * kWaves;
-constexpr int kBins = 2048;   // of one digit of 11, 11 and 10 bits
+constexpr int kBins = 2048;   // of a digit of 11 bits, and of top-p's weights
+constexpr int kList = 2048;   // logits that are sorted in LDS
+constexpr int kTopK = 768;    // the list then has some 1500 logits of a smooth distribution
+constexpr int kStep = 4 * kWave;   // logits of a wave's load
+
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ float widen(float x) { return x; }
 __device__ __forceinline__ float widen(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
 
-// Order-preserving map of the finite and infinite floats to integers (both zeros
-// to one, as they are equal).
+// Order-preserving map of the floats to integers (both zeros to one: they are equal).
 __device__ __forceinline__ uint32_t key_of(float x) {
     const uint32_t u = __float_as_uint(x + 0.f);
     return u & 0x80000000u ? ~u : u | 0x80000000u;
@@ -41,29 +58,26 @@ __device__ __forceinline__ float value_of(uint32_t key) {
 
 template <typename V, typename Op>
 __device__ __forceinline__ V wave_reduce(V x, Op op) {
+#pragma unroll
     for (int m = 1; m < kWave; m *= 2) x = op(x, __shfl_xor(x, m));
     return x;
 }
+template <typename V>
+__device__ __forceinline__ V wave_scan(V x) {   // inclusive sums over the lanes
+    const int lane = (int)threadIdx.x & 63;
+#pragma unroll
+    for (int m = 1; m < kWave; m *= 2) {
+        const V o = __shfl_up(x, m);
+        if (lane >= m) x += o;
+    }
+    return x;
+}
 
-// What is kept of a row: logits above the threshold, and those equal to it up to
-// an index.
-struct Cut {
-    uint32_t key;
-    int last;
-    __device__ __forceinline__ bool keeps(uint32_t k, int i) const { return k > key || (k == key && i <= last); }
-};
+struct Add { template <typename V> __device__ V operator()(V a, V b) const { return a + b; } };
+struct Max { __device__ float operator()(float a, float b) const { return fmaxf(a, b); } };
+struct Min { __device__ int operator()(int a, int b) const { return a < b ? a : b; } };
 
-struct Shared {
-    unsigned long long hist[kBins];
-    unsigned long long part[kWaves];
-    double sum[kWaves];
-    float fmax[kWaves];
-    int ints[kWaves];
-    unsigned long long above, in_bin;
-    int bin, pick;
-    double before;
-};
-
+// Reduction over the workgroup; part: kWaves words of LDS that nothing else uses meanwhile.
 template <typename V, typename Op>
 __device__ V block_reduce(V x, V *part, Op op) {
     x = wave_reduce(x, op);
@@ -71,177 +85,407 @@ __device__ V block_reduce(V x, V *part, Op op) {
     if ((threadIdx.x & 63) == 0) part[threadIdx.x / kWave] = x;
     __syncthreads();
     V y = part[0];
+#pragma unroll
     for (int w = 1; w < kWaves; ++w) y = op(y, part[w]);
     return y;
 }
+// Inclusive sums over the threads.
+template <typename V>
+__device__ V block_scan(V x, V *part) {
+    const int w = (int)threadIdx.x / kWave;
+    x = wave_scan(x);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 63) part[w] = x;
+    __syncthreads();
+    V base = 0;
+    for (int i = 0; i < w; ++i) base += part[i];
+    return base + x;
+}
 
-// The row as the workgroup walks it: wave w has the logits [w * span, (w+1) * span).
-template <typename T>
+// What is kept of a row: the logits above the threshold, and those equal to it up
+// to an index.
+struct Cut {
+    float x;
+    int last;
+    __device__ __forceinline__ bool keeps(float v, int i) const { return v > x || (v == x && i <= last); }
+};
+
+// Weights exp((x - top) / T), to some 4e-14 of themselves: 2^y with y split into a
+// whole number and a rest f of at most a half, 2^f = 1 + f q(f) with q the
+// interpolation of (2^f - 1) / f in the nine Chebyshev nodes.  The weight of top
+// is exactly 1, that of -inf 0.
+struct Mass {
+    double top, c;   // the largest logit; log2(e) / T
+    double unit;     // of whole(): 2^-44 of the largest weight (2^-38 for 2^24 logits)
+    __device__ __forceinline__ double log2w(float x) const { return ((double)x - top) * c; }
+    static __device__ __forceinline__ double exp2_of(double y) {
+        y = fmax(y, -2000.0);   // 0 below; -inf and NaN (of -inf at T = inf) too
+        constexpr double kRound = 6755399441055744.0;   // 1.5 * 2^52: its sum with y has y's whole part in its low bits
+        const double z = y + kRound;
+        const double f = y - (z - kRound);
+        double q = 0x1.b63880a30e9ffp-24;
+        q = fma(q, f, 0x1.63d136366db24p-20);
+        q = fma(q, f, 0x1.ffcb9515a8016p-17);
+        q = fma(q, f, 0x1.4308ac85aa947p-13);
+        q = fma(q, f, 0x1.5d87fe86fe88ep-10);
+        q = fma(q, f, 0x1.3b2ab7181b755p-7);
+        q = fma(q, f, 0x1.c6b08d7047e52p-5);
+        q = fma(q, f, 0x1.ebfbdff823cedp-3);
+        q = fma(q, f, 0x1.62e42fefa39efp-1);
+        return ldexp(fma(q, f, 1.0), (int)(uint32_t)__builtin_bit_cast(unsigned long long, z));
+    }
+    __device__ __forceinline__ double w(float x) const { return exp2_of(log2w(x)); }
+    // as whole numbers, whose sums do not depend on the order of atomic additions
+    __device__ __forceinline__ unsigned long long whole_of(double w) const { return (unsigned long long)(w * unit + 0.5); }
+    __device__ __forceinline__ unsigned long long whole(float x) const { return whole_of(w(x)); }
+};
+
+struct Shared {
+    unsigned long long hist[kBins];   // also the sorted list's weights
+    unsigned long long list[kList];   // key << 32 | ~index: sorted by falling value, then index
+    unsigned long long part[kWaves];
+    double sum[kWaves];
+    float fpart[kWaves];
+    int ints[kWaves];
+    unsigned long long above;
+    int bin, count, pick;
+};
+
+// The row, wave w's part being [w * span, (w + 1) * span): NV loads of four logits
+// a lane in registers, further ones read by each pass.
+template <typename T, int NV>
 struct Row {
     const T *x;
-    int V, span, begin, end;
-    __device__ Row(const T *p, int V_) : x(p), V(V_) {
-        span = (V + kWaves * kWave - 1) / (kWaves * kWave) * kWave;
-        const long long b = (long long)(threadIdx.x / kWave) * span;
-        begin = b < V ? (int)b : V;
-        end = V - begin < span ? V : begin + span;
+    int V, begin, steps;   // of the wave
+    f32x4_t v[NV];
+
+    __device__ __forceinline__ f32x4_t load(int i) const {   // logits i .. i + 3, -inf past the end
+        f32x4_t r;
+        if (i + 4 <= V) {
+            struct __attribute__((packed, aligned(sizeof(T)))) Four { T e[4]; };
+            const Four f = *reinterpret_cast<const Four *>(x + i);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) r[e] = widen(f.e[e]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) r[e] = i + e < V ? widen(x[i + e]) : -INFINITY;
+        }
+        return r;
+    }
+    __device__ __forceinline__ Row(const T *p, int V_) : x(p), V(V_) {
+        const int span = (V + kWaves * kStep - 1) / (kWaves * kStep) * kStep;
+        begin = (int)threadIdx.x / kWave * span;
+        steps = begin >= V ? 0 : ((V - begin < span ? V - begin : span) + kStep - 1) / kStep;
+        const int at = begin + 4 * ((int)threadIdx.x & 63);
+#pragma unroll
+        for (int s = 0; s < NV; ++s) v[s] = f32x4_t{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int s = 0; s < NV; ++s)
+            if (s < steps) v[s] = load(at + s * kStep);
+    }
+    // f(four logits, index of the first); every lane of a wave takes every step
+    template <typename F>
+    __device__ __forceinline__ void each4(F f) const {
+        const int at = begin + 4 * ((int)threadIdx.x & 63);
+#pragma unroll
+        for (int s = 0; s < NV; ++s)
+            if (s < steps) f(v[s], at + s * kStep);
+        for (int s = NV; s < steps; ++s) f(load(at + s * kStep), at + s * kStep);
     }
     template <typename F>
-    __device__ __forceinline__ void each(F f) const {   // f(logit, index); every lane of a wave takes every step
-        for (int i = begin; i < end; i += kWave) {
-            const int j = i + (int)(threadIdx.x & 63);
-            f(j < end ? widen(x[j]) : -INFINITY, j < end ? j : V);
-        }
+    __device__ __forceinline__ void each(F f) const {
+        each4([&](const f32x4_t &q, int i) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) f(q[e], i + e);
+        });
     }
 };
 
-// Weights as whole numbers of 2^-bits of the largest: their sums do not depend
-// on the order of the atomic additions.
-struct Mass {
-    double top, c;      // the largest logit; log2(e) / T
-    double unit;        // 2^bits
-    __device__ __forceinline__ double w(float x) const { return exp2(((double)x - top) * c); }
-    __device__ __forceinline__ unsigned long long whole(float x) const { return (unsigned long long)(w(x) * unit + 0.5); }
-};
+// The bin, counted from bin 0 of `bins`, in which the running sum of sh.hist first
+// reaches target: sh.bin and the sum before it, sh.above; sh.bin = -1 if none does.
+// DOWN: the bins are counted from the last one.
+template <bool DOWN>
+__device__ void find_bin(Shared &sh, int bins, unsigned long long above, unsigned long long target) {
+    const int tid = (int)threadIdx.x;
+    if (tid == 0) sh.bin = -1;
+    const int b0 = 2 * tid, at0 = DOWN ? bins - 1 - b0 : b0, at1 = DOWN ? at0 - 1 : at0 + 1;
+    const unsigned long long a = b0 < bins ? sh.hist[at0] : 0, b = b0 + 1 < bins ? sh.hist[at1] : 0;
+    const unsigned long long p2 = above + block_scan(a + b, sh.part), p1 = p2 - b, p0 = p1 - a;
+    if (p0 < target && target <= p1) sh.bin = at0, sh.above = p0;
+    if (p1 < target && target <= p2) sh.bin = at1, sh.above = p1;
+    __syncthreads();
+}
 
-// The cut at which the sum of f over the kept logits, in the order, first reaches
-// `target` (1 <= target <= the sum over `from`), by digits of the key, the
-// highest first.  f: 1 (counts) or the weight (f is the same for equal logits).
-template <typename T, typename F>
-__device__ Cut find_cut(Shared &sh, const Row<T> &row, const Cut &from, unsigned long long target, F f) {
+__device__ __forceinline__ void clear_bins(Shared &sh) {
+    __syncthreads();
+#pragma unroll
+    for (int b = 0; b < kBins; b += kBlock) sh.hist[b + threadIdx.x] = 0;
+    __syncthreads();
+}
+
+// The cut at which the sum of f over the logits that `from` keeps, in the order,
+// first reaches `target` (1 <= target <= the sum), by digits of the key, the
+// highest first.  f: 1 (counts) or the weight (equal logits have one f).
+template <typename R, typename F>
+__device__ __forceinline__ Cut find_cut(Shared &sh, const R &row, const Cut &from, unsigned long long target, F f) {
     uint32_t prefix = 0, mask = 0;
     unsigned long long above = 0;
     const int tid = (int)threadIdx.x;
     for (int level = 0; level < 3; ++level) {
         const int shift = level == 0 ? 21 : level == 1 ? 10 : 0, bins = level == 2 ? 1024 : 2048;
-        __syncthreads();
-        for (int b = tid; b < kBins; b += kBlock) sh.hist[b] = 0;
-        __syncthreads();
+        clear_bins(sh);
         row.each([&](float x, int i) {
             const uint32_t k = key_of(x);
-            if (i < row.V && (k & mask) == prefix && from.keeps(k, i)) {
+            if ((k & mask) == prefix && from.keeps(x, i)) {
                 const unsigned long long v = f(x);
                 if (v) atomicAdd(&sh.hist[(k >> shift) & (bins - 1)], v);
             }
         });
         __syncthreads();
-        // bins from the highest: thread t has bins bins-1-2t and bins-2-2t
-        const int hi = bins - 1 - 2 * tid;
-        const unsigned long long a = hi >= 0 ? sh.hist[hi] : 0, b = hi >= 1 ? sh.hist[hi - 1] : 0;
-        unsigned long long inc = a + b;
-        for (int m = 1; m < kWave; m *= 2) {
-            const unsigned long long o = __shfl_up(inc, m);
-            if ((tid & 63) >= m) inc += o;
-        }
-        if ((tid & 63) == 63) sh.part[tid / kWave] = inc;
-        __syncthreads();
-        unsigned long long base = above;
-        for (int w = 0; w < tid / kWave; ++w) base += sh.part[w];
-        const unsigned long long p1 = base + inc - b, p0 = p1 - a, p2 = base + inc;   // before a, after a, after b
-        if (p0 < target && target <= p1) sh.bin = hi, sh.above = p0, sh.in_bin = a;
-        if (p1 < target && target <= p2) sh.bin = hi - 1, sh.above = p1, sh.in_bin = b;
-        __syncthreads();
+        find_bin<true>(sh, bins, above, target);
         prefix |= (uint32_t)sh.bin << shift;
         mask |= (uint32_t)(bins - 1) << shift;
         above = sh.above;
+        __syncthreads();
     }
     // the logits equal to the threshold: as many as reach the target, by index
-    const unsigned long long each = f(value_of(prefix));
-    const int need = (int)((target - above + each - 1) / each);
+    const float xt = value_of(prefix);
+    const unsigned long long one = f(xt);
+    const int need = (int)((target - above + one - 1) / one);
     int mine = 0;
-    row.each([&](float x, int i) { mine += i < row.V && key_of(x) == prefix && from.keeps(prefix, i); });
-    mine = wave_reduce(mine, [](int p, int q) { return p + q; });
-    __syncthreads();
-    if ((tid & 63) == 0) sh.ints[tid / kWave] = mine;
+    row.each([&](float x, int i) { mine += x == xt && from.keeps(x, i); });
+    const int upto = wave_reduce(mine, Add{});
+    if ((tid & 63) == 0) sh.ints[tid / kWave] = upto;
     if (tid == 0) sh.pick = row.V;
     __syncthreads();
-    int before = 0;
-    for (int w = 0; w < tid / kWave; ++w) before += sh.ints[w];
-    if (before < need && need <= before + mine) {   // the wave that holds the last one
-        int seen = before;
-        row.each([&](float x, int i) {
-            const bool eq = i < row.V && key_of(x) == prefix && from.keeps(prefix, i);
-            const unsigned long long all = __ballot(eq);
-            const int rank = seen + __popcll(all & ((1ull << (tid & 63)) - 1));
-            if (eq && rank == need - 1) sh.pick = i;
-            seen += __popcll(all);
+    int seen = 0;
+    for (int w = 0; w < tid / kWave; ++w) seen += sh.ints[w];
+    if (seen < need && need <= seen + upto) {   // the wave that has the last one
+        row.each4([&](const f32x4_t &q, int i) {
+            int m = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) m += q[e] == xt && from.keeps(q[e], i + e);
+            const int after = wave_scan(m);
+            int rank = seen + after - m;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (q[e] == xt && from.keeps(q[e], i + e) && ++rank == need) sh.pick = i + e;
+            seen += __shfl(after, 63);
         });
     }
     __syncthreads();
-    return Cut{prefix, sh.pick};
+    return Cut{xt, sh.pick};
 }
 
-template <typename T>
+// Collects the logits for which is(x, i) into sh.list and sorts them; their number
+// (more than kList: the list is not complete, and not sorted).
+template <typename R, typename F>
+__device__ __forceinline__ int sorted_list(Shared &sh, const R &row, F is) {
+    const int tid = (int)threadIdx.x;
+    __syncthreads();
+    if (tid == 0) sh.count = 0;
+    __syncthreads();
+    row.each4([&](const f32x4_t &q, int i) {
+        bool hit[4], any = false;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) hit[e] = is(q[e], i + e), any |= hit[e];
+        if (__any(any)) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (hit[e]) {
+                    const int at = atomicAdd(&sh.count, 1);
+                    if (at < kList) sh.list[at] = (unsigned long long)key_of(q[e]) << 32 | (uint32_t)~(i + e);
+                }
+        }
+    });
+    __syncthreads();
+    const int n = sh.count;
+    if (n > kList) return n;
+    int size = 2;
+    while (size < n) size *= 2;
+    for (int i = n + tid; i < size; i += kBlock) sh.list[i] = 0;   // below every entry
+    __syncthreads();
+    // Bitonic, falling; thread t has one pair.  Pairs less than 64 apart stay inside
+    // the 128 entries of the thread's wave, whose LDS accesses are in order.
+    const int t = tid;
+    for (int k = 2; k <= size; k *= 2) {
+        for (int j = k / 2; j > 0; j /= 2) {
+            const int a = 2 * t - (t & (j - 1)), b = a + j;
+            if (b < size) {
+                const unsigned long long x = sh.list[a], y = sh.list[b];
+                if ((x < y) == ((a & k) == 0)) sh.list[a] = y, sh.list[b] = x;
+            }
+            if (j >= 128 || (j == 1 && k >= 128)) __syncthreads();
+            else if (j == 64) __syncthreads();
+            else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"), __builtin_amdgcn_wave_barrier();
+        }
+    }
+    __syncthreads();
+    return n;
+}
+
+// A key that at least k of the threads' maxima reach (k <= kBlock): the lower end
+// of the digits of 22 bits that the k-th largest one has.
+__device__ uint32_t bound_of(Shared &sh, uint32_t key, int k) {
+    uint32_t prefix = 0, mask = 0;
+    unsigned long long above = 0;
+    for (int level = 0; level < 2; ++level) {
+        const int shift = level == 0 ? 21 : 10;
+        clear_bins(sh);
+        if ((key & mask) == prefix) atomicAdd(&sh.hist[(key >> shift) & (kBins - 1)], 1ull);
+        __syncthreads();
+        find_bin<true>(sh, kBins, above, (unsigned long long)k);
+        prefix |= (uint32_t)sh.bin << shift;
+        mask |= (uint32_t)(kBins - 1) << shift;
+        above = sh.above;
+        __syncthreads();
+    }
+    return prefix;
+}
+
+// The cut of min-p: w >= m where (x - top) c >= log2 m; the least such float, at most top.
+__device__ Cut cut_of_min_p(const Mass &mass, float m, float top, int V) {
+    const double least = log2(fmin((double)m, 1.0));
+    float f = (float)(mass.top + least / mass.c);
+    if (mass.log2w(f) < least) f = nextafterf(f, INFINITY);
+    else if (f > -INFINITY && mass.log2w(nextafterf(f, -INFINITY)) >= least) f = nextafterf(f, -INFINITY);
+    return Cut{f > top ? top : f, V};
+}
+
+template <typename T, int NV>
 __global__ __launch_bounds__(kBlock) void token_sample_kernel(TokenSample a)
 {
     __shared__ Shared sh;
-    const int r = blockIdx.x, tid = (int)threadIdx.x;
-    const Row<T> row(static_cast<const T *>(a.logits) + (size_t)r * a.ld, a.V);
+    const int r = blockIdx.x, tid = (int)threadIdx.x, lane = tid & 63, wv = tid / kWave, V = a.V;
     const float temp = a.temperature ? a.temperature[r] : 1.f;
     const int k = a.top_k ? a.top_k[r] : 0;
     const float p = a.top_p ? a.top_p[r] : 1.f, mp = a.min_p ? a.min_p[r] : 0.f, u = a.u[r];
+    const Row<T, NV> row(static_cast<const T *>(a.logits) + (size_t)r * a.ld, V);
 
-    float top = -INFINITY;
-    int bad = 0;
+    float own = -INFINITY;
+    bool bad = false;
     row.each([&](float x, int) {
-        top = fmaxf(top, x);
+        own = fmaxf(own, x);
         bad |= !(x < INFINITY);
     });
-    top = block_reduce(top, sh.fmax, [](float p, float q) { return fmaxf(p, q); });
-    bad = block_reduce(bad, sh.ints, [](int p, int q) { return p | q; });
-    if (bad || top == -INFINITY || !(temp >= 0.f)) {   // no distribution
+    // a NaN or +inf logit goes through the maximum as +inf
+    const float top = block_reduce(bad ? INFINITY : own, sh.fpart, Max{});
+    if (!(fabsf(top) < INFINITY) || !(temp >= 0.f)) {   // no distribution
         if (tid == 0) a.token[r] = -1, a.logprob[r] = NAN;
         return;
     }
     if (temp == 0.f) {
-        int at = a.V;
-        row.each([&](float x, int i) { at = x == top && i < at ? i : at; });
-        at = block_reduce(at, sh.ints, [](int p, int q) { return p < q ? p : q; });
+        int at = V;
+        if (own == top) row.each([&](float x, int i) { at = x == top && i < at ? i : at; });
+        at = block_reduce(at, sh.ints, Min{});
         if (tid == 0) a.token[r] = at, a.logprob[r] = 0.f;
         return;
     }
     int lg = 0;
-    while (lg < 31 && (1ll << lg) < a.V) ++lg;
+    while (lg < 31 && (1ll << lg) < V) ++lg;
     const Mass mass{(double)top, 1.4426950408889634 / (double)temp, ldexp(1.0, lg > 18 ? 62 - lg : 44)};
 
-    Cut cut{key_of(-INFINITY) + 1, a.V};   // every finite logit
-    if (k > 0 && k < a.V) {
+    Cut cut{-INFINITY, -1};   // every finite logit
+    bool cut_k = k > 0 && k < V, cut_p = p < 1.f;
+    if (cut_k && k <= kTopK) {
+        const uint32_t bound = bound_of(sh, key_of(own), k);
+        const int n = sorted_list(sh, row, [&](float x, int) { return x > -INFINITY && key_of(x) >= bound; });
+        if (n <= kList) {
+            // n >= k unless fewer logits are finite.  Two entries a thread: weights and running sums.
+            const int kept = n < k ? n : k;
+            double *run = reinterpret_cast<double *>(sh.hist);
+            auto value = [&](int i) { return value_of((uint32_t)(sh.list[i] >> 32)); };
+            const double w0 = 2 * tid < kept ? mass.w(value(2 * tid)) : 0.0;
+            const double w1 = 2 * tid + 1 < kept ? mass.w(value(2 * tid + 1)) : 0.0;
+            const double after = block_scan(w0 + w1, sh.sum);
+            run[2 * tid] = after - w1, run[2 * tid + 1] = after;
+            __syncthreads();
+            const double goal_p = (double)fmaxf(p, 0.f) * run[kept - 1];
+            int left = 0;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int i = 2 * tid + e;
+                left += i < kept && (i == 0 || !cut_p || run[i - 1] < goal_p);
+            }
+            left = block_reduce(left, sh.ints, Add{});
+            const unsigned long long at = sh.list[left - 1];
+            cut = Cut{value_of((uint32_t)(at >> 32)), (int)~(uint32_t)at};
+            cut_k = cut_p = false;
+        }
+    }
+    if (cut_k) {
         int live = 0;
         row.each([&](float x, int) { live += x > -INFINITY; });
-        live = block_reduce(live, sh.ints, [](int p, int q) { return p + q; });
+        live = block_reduce(live, sh.ints, Add{});
         if (k < live) cut = find_cut(sh, row, cut, (unsigned long long)k, [](float) { return 1ull; });
     }
-    if (p < 1.f) {
-        unsigned long long all = 0;
-        row.each([&](float x, int i) { all += cut.keeps(key_of(x), i) ? mass.whole(x) : 0ull; });
-        all = block_reduce(all, sh.part, [](unsigned long long p, unsigned long long q) { return p + q; });
-        const double t = ceil((double)fmaxf(p, 0.f) * (double)all);
-        unsigned long long target = t < 1.0 ? 1ull : (unsigned long long)t;
-        if (target > all) target = all;
-        cut = find_cut(sh, row, cut, target, [&](float x) { return mass.whole(x); });
+    if (cut_p) {
+        // the weights below 2^-deep, all together, have less than half of 1 - p
+        const double deep = log2((double)V / (1.0 - (double)fmaxf(p, 0.f))) + 1.0, per = kBins / deep;
+        clear_bins(sh);
+        double all = 0.0;
+        row.each4([&](const f32x4_t &q, int i) {
+            if (!__any(cut.keeps(q[0], i) || cut.keeps(q[1], i + 1) || cut.keeps(q[2], i + 2) || cut.keeps(q[3], i + 3))) return;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (!cut.keeps(q[e], i + e)) continue;
+                const double y = mass.log2w(q[e]), w = Mass::exp2_of(y), b = -y * per;
+                all += w;
+                if (b < kBins) atomicAdd(&sh.hist[(int)b], mass.whole_of(w));
+            }
+        });
+        all = block_reduce(all, sh.sum, Add{});
+        const double t = ceil((double)fmaxf(p, 0.f) * all * mass.unit);
+        const unsigned long long target = t < 1.0 ? 1ull : (unsigned long long)t;
+        find_bin<false>(sh, kBins, 0, target);
+        const int bin = sh.bin;
+        const unsigned long long above = sh.above;
+        int n = kList + 1;
+        if (bin >= 0)
+            n = sorted_list(sh, row, [&](float x, int i) {
+                const double b = -mass.log2w(x) * per;
+                return cut.keeps(x, i) && b < kBins && (int)b == bin;
+            });
+        if (n <= kList) {
+            auto value = [&](int i) { return value_of((uint32_t)(sh.list[i] >> 32)); };
+            const unsigned long long w0 = 2 * tid < n ? mass.whole(value(2 * tid)) : 0;
+            const unsigned long long w1 = 2 * tid + 1 < n ? mass.whole(value(2 * tid + 1)) : 0;
+            const unsigned long long p2 = above + block_scan(w0 + w1, sh.part), p1 = p2 - w1, p0 = p1 - w0;
+            const int hit = p0 < target && target <= p1 ? 2 * tid : p1 < target && target <= p2 ? 2 * tid + 1 : -1;
+            if (hit >= 0) sh.pick = hit;
+            __syncthreads();
+            const unsigned long long at = sh.list[sh.pick];
+            cut = Cut{value_of((uint32_t)(at >> 32)), (int)~(uint32_t)at};
+        } else {   // more of one value, or nearly, than the list takes
+            unsigned long long whole = 0;
+            row.each([&](float x, int i) { whole += cut.keeps(x, i) ? mass.whole(x) : 0ull; });
+            whole = block_reduce(whole, sh.part, Add{});
+            cut = find_cut(sh, row, cut, target < whole ? target : whole, [&](float x) { return mass.whole(x); });
+        }
     }
-    if (mp > 0.f && mass.c > 0.0) {   // w >= m where (x - top) * c >= log2 m
-        const double least = log2(fmin((double)mp, 1.0));
-        // the least logit that passes: the threshold as a float, rounded up
-        double xt = mass.top + least / mass.c;
-        float f = (float)xt;
-        if (((double)f - mass.top) * mass.c < least) f = nextafterf(f, INFINITY);
-        else if (f > -INFINITY && ((double)nextafterf(f, -INFINITY) - mass.top) * mass.c >= least) f = nextafterf(f, -INFINITY);
-        if (f > top) f = top;
-        if (key_of(f) > cut.key) cut = Cut{key_of(f), a.V};
+    if (mp > 0.f && mass.c > 0.0) {
+        const Cut c = cut_of_min_p(mass, mp, top, V);
+        if (c.x > cut.x) cut = c;
     }
 
-    // the draw: the waves' sums, then the one wave that holds the token
+    // the draw: the waves' sums, the wave that has the token, the sums of parts of its part
     double mine = 0.0;
-    row.each([&](float x, int i) { mine += i < a.V && cut.keeps(key_of(x), i) ? mass.w(x) : 0.0; });
-    mine = wave_reduce(mine, [](double p, double q) { return p + q; });
+    row.each4([&](const f32x4_t &q, int i) {
+        bool kept[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) kept[e] = cut.keeps(q[e], i + e);
+        if (!__any(kept[0] || kept[1] || kept[2] || kept[3])) return;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) mine += kept[e] ? mass.w(q[e]) : 0.0;
+    });
+    mine = wave_reduce(mine, Add{});
     __syncthreads();
-    if ((tid & 63) == 0) sh.sum[tid / kWave] = mine;
+    if (lane == 0) sh.sum[wv] = mine;
     __syncthreads();
     double total = 0.0;
     for (int w = 0; w < kWaves; ++w) total += sh.sum[w];
     const double goal = (double)u * total;
-    int holder = -1;
+    int holder = 0;
     double before = 0.0, run = 0.0;
     for (int w = 0; w < kWaves; ++w) {
         if (sh.sum[w] > 0.0) {
@@ -250,26 +494,68 @@ __global__ __launch_bounds__(kBlock) void token_sample_kernel(TokenSample a)
         }
         run += sh.sum[w];
     }
-    if (tid / kWave != holder) return;
+    __syncthreads();
+    // its part in kWaves parts of whole loads
+    const int span = (V + kWaves * kStep - 1) / (kWaves * kStep) * kStep;
+    const int steps = (span / kStep + kWaves - 1) / kWaves;
+    const int first = holder * span + wv * steps * kStep, stop = (holder + 1) * span;
+    auto weights = [&](int s, double (&w)[4], int &i) {
+        i = first + s * kStep + 4 * lane;
+        const bool in = first + s * kStep < stop && i < V;
+        const f32x4_t q = in ? row.load(i) : f32x4_t{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = cut.keeps(q[e], i + e) ? mass.w(q[e]) : 0.0;
+    };
+    mine = 0.0;
+    for (int s = 0; s < steps; ++s) {
+        double w[4];
+        int i;
+        weights(s, w, i);
+        mine += (w[0] + w[1]) + (w[2] + w[3]);
+    }
+    mine = wave_reduce(mine, Add{});
+    if (lane == 0) sh.sum[wv] = mine;
+    __syncthreads();
+    int sub = 0;
+    run = before;
+    for (int w = 0; w < kWaves; ++w) {
+        if (sh.sum[w] > 0.0) {
+            sub = w, before = run;
+            if (run + sh.sum[w] > goal) break;
+        }
+        run += sh.sum[w];
+    }
+    if (wv != sub) return;
     int at = -1;
     double w_at = 0.0, seen = before;
     bool done = false;
-    row.each([&](float x, int i) {
-        const double w = i < a.V && cut.keeps(key_of(x), i) ? mass.w(x) : 0.0;
-        double inc = w;
-        for (int m = 1; m < kWave; m *= 2) {
-            const double o = __shfl_up(inc, m);
-            if ((tid & 63) >= m) inc += o;
+    for (int s = 0; s < steps && !done; ++s) {
+        double w[4];
+        int i;
+        weights(s, w, i);
+        const double sum = (w[0] + w[1]) + (w[2] + w[3]), after = wave_scan(sum);
+        double x = seen + (after - sum);
+        int hit = -1, last = -1;
+        double w_hit = 0.0, w_last = 0.0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            x += w[e];
+            if (w[e] > 0.0) {
+                last = e, w_last = w[e];
+                if (hit < 0 && x > goal) hit = e, w_hit = w[e];
+            }
         }
-        const unsigned long long has = __ballot(w > 0.0), past = __ballot(w > 0.0 && seen + inc > goal);
-        if (!done && has) {
-            const int lane = past ? __ffsll((long long)past) - 1 : 63 - __clzll((long long)has);
-            at = __shfl(i, lane), w_at = __shfl(w, lane);
-            done = past != 0;
+        const unsigned long long past = __ballot(hit >= 0), has = __ballot(last >= 0);
+        if (past) {
+            const int l = __ffsll((long long)past) - 1;
+            at = __shfl(i + hit, l), w_at = __shfl(w_hit, l), done = true;
+        } else if (has) {   // the last one, if no later sum passes
+            const int l = 63 - __clzll((long long)has);
+            at = __shfl(i + last, l), w_at = __shfl(w_last, l);
         }
-        seen += __shfl(inc, 63);
-    });
-    if ((tid & 63) == 0) a.token[r] = at, a.logprob[r] = (float)log(w_at / total);
+        seen += __shfl(after, 63);
+    }
+    if (lane == 0) a.token[r] = at, a.logprob[r] = (float)log(w_at / total);
 }
 
 }  // namespace
@@ -278,8 +564,12 @@ size_t token_sample_workspace_bytes(int, int, int) { return 16; }
 
 hipError_t launch_token_sample(const TokenSample &a, bool bf16, hipStream_t stream)
 {
-    if (bf16) hipLaunchKernelGGL(token_sample_kernel<uint16_t>, dim3((unsigned)a.R), dim3(kBlock), 0, stream, a);
-    else hipLaunchKernelGGL(token_sample_kernel<float>, dim3((unsigned)a.R), dim3(kBlock), 0, stream, a);
+    const dim3 gd((unsigned)a.R), bd(kBlock);
+    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, gd, bd, 0, stream, a); };
+    // as few registers as the row needs
+    const int steps = (a.V + kWaves * kStep - 1) / (kWaves * kStep);
+    if (steps <= 4) bf16 ? launch(token_sample_kernel<uint16_t, 4>) : launch(token_sample_kernel<float, 4>);
+    else bf16 ? launch(token_sample_kernel<uint16_t, 16>) : launch(token_sample_kernel<float, 16>);
     return hipGetLastError();
 }
 
