@@ -188,8 +188,13 @@ struct Row {
     __device__ __forceinline__ void each4(F f) const {
         const int at = begin + 4 * ((int)threadIdx.x & 63);
 #pragma unroll
-        for (int s = 0; s < NV; ++s)
-            if (s < steps) f(v[s], at + s * kStep);
+        for (int s = 0; s < NV; ++s) {
+            // The row leaves few registers: nothing that one pass derives from it (keys,
+            // differences in 64 bits) may be kept for the next.
+            f32x4_t q = v[s];
+            asm volatile("" : "+v"(q[0]), "+v"(q[1]), "+v"(q[2]), "+v"(q[3]));
+            if (s < steps) f(q, at + s * kStep);
+        }
         for (int s = NV; s < steps; ++s) f(load(at + s * kStep), at + s * kStep);
     }
     template <typename F>
