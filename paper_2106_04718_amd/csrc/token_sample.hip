@@ -15,14 +15,18 @@
 // vocabulary has many borders: with the weights in 32 bits one draw in some ten
 // thousand would be another token's.  Weights and sums are 64-bit.
 //
-// One workgroup has a row, in registers up to 65536 logits (more are read again
-// by each pass).  No pass sorts or scans the row:
+// One workgroup has a row and reads it two or three times, after the first time
+// from the caches (held in registers, it needs unrolled passes, which run once a
+// row: waiting for their instructions cost more than reading again).  No pass
+// sorts or scans the row:
 //   top-k      The k-th largest of the threads' 1024 maxima is a bound that at
 //              least k logits reach, and few more do.  Those go to a list in LDS,
 //              which is sorted; top-p, min-p and the draw happen in the list.
 //   top-p      alone: one pass adds up all weights, and those that can matter
 //              (together the others have less than half of 1 - p) by value, in
-//              2048 bins.  The list is the bin in which the mass reaches p.
+//              2048 bins.  The list has the logits down to the bin in which the
+//              mass reaches p; the draw happens in it.  If they are too many, the
+//              list has that bin alone, for the cut.
 //   otherwise  (no cut, or the list's capacity exceeded, or k above kTopK) the cut
 //              is found by digits of the logits' bits, and the draw by the waves'
 //              sums and the part of the row of the wave that holds it.
@@ -41,6 +45,7 @@ constexpr int kBins = 2048;   // of a digit of 11 bits, and of top-p's weights
 constexpr int kList = 2048;   // logits that are sorted in LDS
 constexpr int kTopK = 768;    // the list then has some 1500 logits of a smooth distribution
 constexpr int kStep = 4 * kWave;   // logits of a wave's load
+constexpr int kAhead = 4;          // loads on their way
 
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 
@@ -56,30 +61,62 @@ __device__ __forceinline__ float value_of(uint32_t key) {
     return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key);
 }
 
+// ---- exchange between lanes ---------------------------------------------------
+// On the words of a value: DPP inside rows of 16 lanes, permlane swaps across them.
+template <typename V, typename F>
+__device__ __forceinline__ V by_words(V x, F f) {
+    if constexpr (sizeof(V) == 4) {
+        return __builtin_bit_cast(V, f(__builtin_bit_cast(uint32_t, x)));
+    } else {
+        const auto u = __builtin_bit_cast(unsigned long long, x);
+        return __builtin_bit_cast(V, (unsigned long long)f((uint32_t)(u >> 32)) << 32 | f((uint32_t)u));
+    }
+}
+template <int CTRL, int ROWS = 0xF, typename V>
+__device__ __forceinline__ V dpp(V x) {   // 0 where the source lane does not exist or the row is masked
+    return by_words(x, [](uint32_t u) {
+        return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)u, CTRL, ROWS, 0xF, CTRL < 0x142 || CTRL > 0x143);
+    });
+}
+template <int MASK, typename V>
+__device__ __forceinline__ V other_row(V x) {   // of lane ^ MASK, MASK = 16 or 32
+    return by_words(x, [](uint32_t u) {
+        const bool up = (__lane_id() & MASK) != 0;
+        if constexpr (MASK == 16) {
+            const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+            return (uint32_t)(up ? r[0] : r[1]);
+        } else {
+            const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+            return (uint32_t)(up ? r[0] : r[1]);
+        }
+    });
+}
 template <typename V, typename Op>
-__device__ __forceinline__ V wave_reduce(V x, Op op) {
-#pragma unroll
-    for (int m = 1; m < kWave; m *= 2) x = op(x, __shfl_xor(x, m));
-    return x;
+__device__ __forceinline__ V wave_reduce(V x, Op op) {   // the same bits in every lane: each step pairs lanes
+    x = op(x, dpp<0xB1>(x));    // lane ^ 1
+    x = op(x, dpp<0x4E>(x));    // lane ^ 2
+    x = op(x, dpp<0x141>(x));   // the other four of eight
+    x = op(x, dpp<0x140>(x));   // the other eight of sixteen
+    x = op(x, other_row<16>(x));
+    return op(x, other_row<32>(x));
 }
 template <typename V>
 __device__ __forceinline__ V wave_scan(V x) {   // inclusive sums over the lanes
-    const int lane = (int)threadIdx.x & 63;
-#pragma unroll
-    for (int m = 1; m < kWave; m *= 2) {
-        const V o = __shfl_up(x, m);
-        if (lane >= m) x += o;
-    }
-    return x;
+    x += dpp<0x111>(x);         // of the row: from 1, 2, 4 and 8 lanes before
+    x += dpp<0x112>(x);
+    x += dpp<0x114>(x);
+    x += dpp<0x118>(x);
+    x += dpp<0x142, 0xA>(x);    // the last of row 0 and 2 to row 1 and 3
+    return x + dpp<0x143, 0xC>(x);   // the last of row 1 to rows 2 and 3
 }
 
 struct Add { template <typename V> __device__ V operator()(V a, V b) const { return a + b; } };
 struct Max { __device__ float operator()(float a, float b) const { return fmaxf(a, b); } };
-struct Min { __device__ int operator()(int a, int b) const { return a < b ? a : b; } };
+struct Min { template <typename V> __device__ V operator()(V a, V b) const { return a < b ? a : b; } };
 
 // Reduction over the workgroup; part: kWaves words of LDS that nothing else uses meanwhile.
 template <typename V, typename Op>
-__device__ V block_reduce(V x, V *part, Op op) {
+__device__ __forceinline__ V block_reduce(V x, V *part, Op op) {
     x = wave_reduce(x, op);
     __syncthreads();
     if ((threadIdx.x & 63) == 0) part[threadIdx.x / kWave] = x;
@@ -91,14 +128,18 @@ __device__ V block_reduce(V x, V *part, Op op) {
 }
 // Inclusive sums over the threads.
 template <typename V>
-__device__ V block_scan(V x, V *part) {
-    const int w = (int)threadIdx.x / kWave;
+__device__ __forceinline__ V block_scan(V x, V *part) {
+    const int wv = (int)threadIdx.x / kWave;
     x = wave_scan(x);
     __syncthreads();
-    if ((threadIdx.x & 63) == 63) part[w] = x;
+    if ((threadIdx.x & 63) == 63) part[wv] = x;
     __syncthreads();
     V base = 0;
-    for (int i = 0; i < w; ++i) base += part[i];
+#pragma unroll
+    for (int w = 0; w < kWaves - 1; ++w) {   // all read at once, no loop of dependent reads
+        const V y = part[w];
+        base += w < wv ? y : V(0);
+    }
     return base + x;
 }
 
@@ -148,54 +189,46 @@ struct Shared {
     float fpart[kWaves];
     int ints[kWaves];
     unsigned long long above;
+    double total;
     int bin, count, pick;
 };
 
-// The row, wave w's part being [w * span, (w + 1) * span): NV loads of four logits
-// a lane in registers, further ones read by each pass.
-template <typename T, int NV>
+// The row, wave w's part being [w * span, (w + 1) * span).
+template <typename T>
 struct Row {
     const T *x;
-    int V, begin, steps;   // of the wave
-    f32x4_t v[NV];
+    int V, begin, end;   // of the wave
 
+    struct __attribute__((packed, aligned(sizeof(T)))) Four { T e[4]; };   // rows begin at any element
+    static __device__ __forceinline__ f32x4_t wide(const Four &f) {
+        return f32x4_t{widen(f.e[0]), widen(f.e[1]), widen(f.e[2]), widen(f.e[3])};
+    }
     __device__ __forceinline__ f32x4_t load(int i) const {   // logits i .. i + 3, -inf past the end
+        if (i + 4 <= V) return wide(*reinterpret_cast<const Four *>(x + i));
         f32x4_t r;
-        if (i + 4 <= V) {
-            struct __attribute__((packed, aligned(sizeof(T)))) Four { T e[4]; };
-            const Four f = *reinterpret_cast<const Four *>(x + i);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) r[e] = widen(f.e[e]);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) r[e] = i + e < V ? widen(x[i + e]) : -INFINITY;
-        }
+        for (int e = 0; e < 4; ++e) r[e] = i + e < V ? widen(x[i + e]) : -INFINITY;
         return r;
     }
+    static __device__ __forceinline__ int span_of(int V) { return (V + kWaves * kStep - 1) / (kWaves * kStep) * kStep; }
     __device__ __forceinline__ Row(const T *p, int V_) : x(p), V(V_) {
-        const int span = (V + kWaves * kStep - 1) / (kWaves * kStep) * kStep;
-        begin = (int)threadIdx.x / kWave * span;
-        steps = begin >= V ? 0 : ((V - begin < span ? V - begin : span) + kStep - 1) / kStep;
-        const int at = begin + 4 * ((int)threadIdx.x & 63);
-#pragma unroll
-        for (int s = 0; s < NV; ++s) v[s] = f32x4_t{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-        for (int s = 0; s < NV; ++s)
-            if (s < steps) v[s] = load(at + s * kStep);
+        const int span = span_of(V), w = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
+        begin = w * span < V ? w * span : V;
+        end = V - begin < span ? V : begin + span;
     }
-    // f(four logits, index of the first); every lane of a wave takes every step
+    // f(four logits, index of the first), in the order of the indices; every lane of a wave takes every step
     template <typename F>
     __device__ __forceinline__ void each4(F f) const {
-        const int at = begin + 4 * ((int)threadIdx.x & 63);
+        const int lane4 = 4 * ((int)threadIdx.x & 63);
+        int i = begin;
+        for (; end - i >= kAhead * kStep; i += kAhead * kStep) {   // whole loads, kAhead of them on their way
+            Four q[kAhead];
 #pragma unroll
-        for (int s = 0; s < NV; ++s) {
-            // The row leaves few registers: nothing that one pass derives from it (keys,
-            // differences in 64 bits) may be kept for the next.
-            f32x4_t q = v[s];
-            asm volatile("" : "+v"(q[0]), "+v"(q[1]), "+v"(q[2]), "+v"(q[3]));
-            if (s < steps) f(q, at + s * kStep);
+            for (int s = 0; s < kAhead; ++s) q[s] = *reinterpret_cast<const Four *>(x + i + s * kStep + lane4);
+#pragma unroll
+            for (int s = 0; s < kAhead; ++s) f(wide(q[s]), i + s * kStep + lane4);
         }
-        for (int s = NV; s < steps; ++s) f(load(at + s * kStep), at + s * kStep);
+        for (; i < end; i += kStep) f(load(i + lane4), i + lane4);
     }
     template <typename F>
     __device__ __forceinline__ void each(F f) const {
@@ -264,7 +297,11 @@ __device__ __forceinline__ Cut find_cut(Shared &sh, const R &row, const Cut &fro
     if (tid == 0) sh.pick = row.V;
     __syncthreads();
     int seen = 0;
-    for (int w = 0; w < tid / kWave; ++w) seen += sh.ints[w];
+#pragma unroll
+    for (int w = 0; w < kWaves - 1; ++w) {
+        const int y = sh.ints[w];
+        seen += w < tid / kWave ? y : 0;
+    }
     if (seen < need && need <= seen + upto) {   // the wave that has the last one
         row.each4([&](const f32x4_t &q, int i) {
             int m = 0;
@@ -282,13 +319,12 @@ __device__ __forceinline__ Cut find_cut(Shared &sh, const R &row, const Cut &fro
     return Cut{xt, sh.pick};
 }
 
-// Collects the logits for which is(x, i) into sh.list and sorts them; their number
-// (more than kList: the list is not complete, and not sorted).
+// Collects the logits for which is(x, i) into sh.list; their number (above kList:
+// the list is not complete).
 template <typename R, typename F>
-__device__ __forceinline__ int sorted_list(Shared &sh, const R &row, F is) {
-    const int tid = (int)threadIdx.x;
+__device__ __forceinline__ int collect(Shared &sh, const R &row, F is) {
     __syncthreads();
-    if (tid == 0) sh.count = 0;
+    if (threadIdx.x == 0) sh.count = 0;
     __syncthreads();
     row.each4([&](const f32x4_t &q, int i) {
         bool hit[4], any = false;
@@ -304,15 +340,18 @@ __device__ __forceinline__ int sorted_list(Shared &sh, const R &row, F is) {
         }
     });
     __syncthreads();
-    const int n = sh.count;
-    if (n > kList) return n;
+    return sh.count;
+}
+
+// Sorts the first n entries of sh.list, falling (bitonic; thread t has one pair).
+// Pairs less than 128 apart stay inside the 128 entries of the thread's wave, whose
+// LDS accesses are in order.
+__device__ __forceinline__ void sort_list(Shared &sh, int n) {
+    const int t = (int)threadIdx.x;
     int size = 2;
     while (size < n) size *= 2;
-    for (int i = n + tid; i < size; i += kBlock) sh.list[i] = 0;   // below every entry
+    for (int i = n + t; i < size; i += kBlock) sh.list[i] = 0;   // below every entry
     __syncthreads();
-    // Bitonic, falling; thread t has one pair.  Pairs less than 64 apart stay inside
-    // the 128 entries of the thread's wave, whose LDS accesses are in order.
-    const int t = tid;
     for (int k = 2; k <= size; k *= 2) {
         for (int j = k / 2; j > 0; j /= 2) {
             const int a = 2 * t - (t & (j - 1)), b = a + j;
@@ -321,31 +360,47 @@ __device__ __forceinline__ int sorted_list(Shared &sh, const R &row, F is) {
                 if ((x < y) == ((a & k) == 0)) sh.list[a] = y, sh.list[b] = x;
             }
             if (j >= 128 || (j == 1 && k >= 128)) __syncthreads();
-            else if (j == 64) __syncthreads();
             else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"), __builtin_amdgcn_wave_barrier();
         }
     }
     __syncthreads();
-    return n;
 }
+__device__ __forceinline__ float list_value(const Shared &sh, int i) { return value_of((uint32_t)(sh.list[i] >> 32)); }
 
-// A key that at least k of the threads' maxima reach (k <= kBlock): the lower end
-// of the digits of 22 bits that the k-th largest one has.
-__device__ uint32_t bound_of(Shared &sh, uint32_t key, int k) {
-    uint32_t prefix = 0, mask = 0;
-    unsigned long long above = 0;
-    for (int level = 0; level < 2; ++level) {
-        const int shift = level == 0 ? 21 : 10;
-        clear_bins(sh);
-        if ((key & mask) == prefix) atomicAdd(&sh.hist[(key >> shift) & (kBins - 1)], 1ull);
+// A bound that at least k of the threads' maxima reach (k <= kBlock), and not many
+// more: the least of those down to the bin, of 1024 between the largest and the
+// least finite one, in which the k-th is.  Where outliers crowd the others into
+// one bin, again between that bin's ends.
+__device__ __forceinline__ float bound_of(Shared &sh, float own, float top, int k) {
+    uint32_t *count = reinterpret_cast<uint32_t *>(sh.hist), *least = count + kBlock;
+    const int tid = (int)threadIdx.x;
+    float hi = top, lo = block_reduce(own > -INFINITY ? own : top, sh.fpart, Min{}), bound = -INFINITY;
+    int before = 0;
+    for (int level = 0; level < 4; ++level) {
+        count[tid] = 0, least[tid] = 0xffffffffu;
+        if (tid == 0) sh.bin = -1;
         __syncthreads();
-        find_bin<true>(sh, kBins, above, (unsigned long long)k);
-        prefix |= (uint32_t)sh.bin << shift;
-        mask |= (uint32_t)(kBins - 1) << shift;
-        above = sh.above;
+        const float per = (float)kBlock / (hi - lo);   // infinite: all in the first bin, or NaN, which is no bin
+        const float b = (hi - own) * per;
+        const int bin = own == hi ? 0 : b < (float)kBlock ? (int)b : kBlock - 1;
+        const bool in = own >= lo && own <= hi;
+        if (in) atomicAdd(&count[bin], 1u), atomicMin(&least[bin], key_of(own));
+        __syncthreads();
+        const int c = (int)count[tid], upto = before + block_scan(c, sh.ints);
+        if (upto - c < k && k <= upto) sh.bin = tid, sh.above = (unsigned long long)(upto - c) << 32 | (unsigned)c;
+        __syncthreads();
+        if (sh.bin < 0) return -INFINITY;   // fewer than k finite maxima
+        bound = value_of(least[sh.bin]);
+        before = (int)(sh.above >> 32);
+        const int here = (int)(uint32_t)sh.above;
+        if (before + here <= k + k / 4 + 32) break;
+        // the ends of that bin, by its members
+        const float high = block_reduce(in && bin == sh.bin ? own : -INFINITY, sh.fpart, Max{});
+        if (high == bound) break;
+        hi = high, lo = bound;
         __syncthreads();
     }
-    return prefix;
+    return bound;
 }
 
 // The cut of min-p: w >= m where (x - top) c >= log2 m; the least such float, at most top.
@@ -357,15 +412,48 @@ __device__ Cut cut_of_min_p(const Mass &mass, float m, float top, int V) {
     return Cut{f > top ? top : f, V};
 }
 
-template <typename T, int NV>
-__global__ __launch_bounds__(kBlock) void token_sample_kernel(TokenSample a)
+// The draw among the first n entries of the sorted list: in the order of the indices.
+__device__ __forceinline__ void draw_from_list(Shared &sh, const TokenSample &a, const Mass &mass, int r, float u, int n) {
+    const int tid = (int)threadIdx.x;
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < kList; e += kBlock) {
+        const unsigned long long x = sh.list[e + tid];
+        if (e + tid < n) sh.list[e + tid] = x << 32 | x >> 32;   // ~index, key
+    }
+    __syncthreads();
+    sort_list(sh, n);
+    double w[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) w[e] = 2 * tid + e < n ? mass.w(value_of((uint32_t)sh.list[2 * tid + e])) : 0.0;
+    const double p2 = block_scan(w[0] + w[1], sh.sum), p1 = p2 - w[1];
+    if (tid == kBlock - 1) sh.total = p2;
+    if (tid == 0) sh.pick = kList;
+    __syncthreads();
+    const double total = sh.total, goal = (double)u * total;
+    const int hit = w[0] > 0.0 && p1 > goal ? 2 * tid : w[1] > 0.0 && p2 > goal ? 2 * tid + 1 : kList;
+    if (hit < kList) atomicMin(&sh.pick, hit);
+    __syncthreads();
+    int at = sh.pick;
+    if (at == kList) {   // no sum exceeds u's share: the last one
+        const int last = w[1] > 0.0 ? 2 * tid + 1 : w[0] > 0.0 ? 2 * tid : 0;
+        at = -block_reduce(-last, sh.ints, Min{});
+    }
+    if (tid == at / 2) {
+        a.token[r] = (int)~(uint32_t)(sh.list[at] >> 32);
+        a.logprob[r] = (float)log((at & 1 ? w[1] : w[0]) / total);
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kBlock, 8) void token_sample_kernel(TokenSample a)
 {
     __shared__ Shared sh;
     const int r = blockIdx.x, tid = (int)threadIdx.x, lane = tid & 63, wv = tid / kWave, V = a.V;
     const float temp = a.temperature ? a.temperature[r] : 1.f;
     const int k = a.top_k ? a.top_k[r] : 0;
     const float p = a.top_p ? a.top_p[r] : 1.f, mp = a.min_p ? a.min_p[r] : 0.f, u = a.u[r];
-    const Row<T, NV> row(static_cast<const T *>(a.logits) + (size_t)r * a.ld, V);
+    const Row<T> row(static_cast<const T *>(a.logits) + (size_t)r * a.ld, V);
 
     float own = -INFINITY;
     bool bad = false;
@@ -389,33 +477,38 @@ __global__ __launch_bounds__(kBlock) void token_sample_kernel(TokenSample a)
     int lg = 0;
     while (lg < 31 && (1ll << lg) < V) ++lg;
     const Mass mass{(double)top, 1.4426950408889634 / (double)temp, ldexp(1.0, lg > 18 ? 62 - lg : 44)};
+    const Cut cut_m = mp > 0.f && mass.c > 0.0 ? cut_of_min_p(mass, mp, top, V) : Cut{-INFINITY, -1};
 
     Cut cut{-INFINITY, -1};   // every finite logit
     bool cut_k = k > 0 && k < V, cut_p = p < 1.f;
     if (cut_k && k <= kTopK) {
-        const uint32_t bound = bound_of(sh, key_of(own), k);
-        const int n = sorted_list(sh, row, [&](float x, int) { return x > -INFINITY && key_of(x) >= bound; });
+        const float bound = bound_of(sh, own, top, k);
+        const int n = collect(sh, row, [&](float x, int) { return x > -INFINITY && x >= bound; });
         if (n <= kList) {
             // n >= k unless fewer logits are finite.  Two entries a thread: weights and running sums.
+            sort_list(sh, n);
             const int kept = n < k ? n : k;
             double *run = reinterpret_cast<double *>(sh.hist);
-            auto value = [&](int i) { return value_of((uint32_t)(sh.list[i] >> 32)); };
-            const double w0 = 2 * tid < kept ? mass.w(value(2 * tid)) : 0.0;
-            const double w1 = 2 * tid + 1 < kept ? mass.w(value(2 * tid + 1)) : 0.0;
-            const double after = block_scan(w0 + w1, sh.sum);
-            run[2 * tid] = after - w1, run[2 * tid + 1] = after;
+            float x[2];
+            double w[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                x[e] = 2 * tid + e < kept ? list_value(sh, 2 * tid + e) : -INFINITY;
+                w[e] = mass.w(x[e]);
+            }
+            const double after = block_scan(w[0] + w[1], sh.sum);
+            run[2 * tid] = after - w[1], run[2 * tid + 1] = after;
             __syncthreads();
-            const double goal_p = (double)fmaxf(p, 0.f) * run[kept - 1];
+            const double goal = (double)fmaxf(p, 0.f) * run[kept - 1];
             int left = 0;
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const int i = 2 * tid + e;
-                left += i < kept && (i == 0 || !cut_p || run[i - 1] < goal_p);
+                left += i < kept && (i == 0 || !cut_p || run[i - 1] < goal) && x[e] >= cut_m.x;
             }
             left = block_reduce(left, sh.ints, Add{});
-            const unsigned long long at = sh.list[left - 1];
-            cut = Cut{value_of((uint32_t)(at >> 32)), (int)~(uint32_t)at};
-            cut_k = cut_p = false;
+            draw_from_list(sh, a, mass, r, u, left);
+            return;
         }
     }
     if (cut_k) {
@@ -430,7 +523,6 @@ __global__ __launch_bounds__(kBlock) void token_sample_kernel(TokenSample a)
         clear_bins(sh);
         double all = 0.0;
         row.each4([&](const f32x4_t &q, int i) {
-            if (!__any(cut.keeps(q[0], i) || cut.keeps(q[1], i + 1) || cut.keeps(q[2], i + 2) || cut.keeps(q[3], i + 3))) return;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 if (!cut.keeps(q[e], i + e)) continue;
@@ -444,21 +536,39 @@ __global__ __launch_bounds__(kBlock) void token_sample_kernel(TokenSample a)
         const unsigned long long target = t < 1.0 ? 1ull : (unsigned long long)t;
         find_bin<false>(sh, kBins, 0, target);
         const int bin = sh.bin;
-        const unsigned long long above = sh.above;
+        unsigned long long above = 0;
         int n = kList + 1;
-        if (bin >= 0)
-            n = sorted_list(sh, row, [&](float x, int i) {
-                const double b = -mass.log2w(x) * per;
-                return cut.keeps(x, i) && b < kBins && (int)b == bin;
-            });
+        bool whole_nucleus = false;
+        if (bin >= 0) {
+            above = sh.above;
+            for (int from = 0; from <= bin; from += bin ? bin : 1) {   // bins 0 .. bin, or bin alone
+                n = collect(sh, row, [&](float x, int i) {
+                    const double b = -mass.log2w(x) * per;
+                    return cut.keeps(x, i) && b < (double)(bin + 1) && b >= (double)from;
+                });
+                whole_nucleus = from == 0;
+                if (n <= kList) break;
+            }
+        }
         if (n <= kList) {
-            auto value = [&](int i) { return value_of((uint32_t)(sh.list[i] >> 32)); };
-            const unsigned long long w0 = 2 * tid < n ? mass.whole(value(2 * tid)) : 0;
-            const unsigned long long w1 = 2 * tid + 1 < n ? mass.whole(value(2 * tid + 1)) : 0;
-            const unsigned long long p2 = above + block_scan(w0 + w1, sh.part), p1 = p2 - w1, p0 = p1 - w0;
+            sort_list(sh, n);
+            unsigned long long w[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) w[e] = 2 * tid + e < n ? mass.whole(list_value(sh, 2 * tid + e)) : 0;
+            const unsigned long long p2 = (whole_nucleus ? 0 : above) + block_scan(w[0] + w[1], sh.part);
+            const unsigned long long p1 = p2 - w[1], p0 = p1 - w[0];
             const int hit = p0 < target && target <= p1 ? 2 * tid : p1 < target && target <= p2 ? 2 * tid + 1 : -1;
             if (hit >= 0) sh.pick = hit;
             __syncthreads();
+            if (whole_nucleus) {
+                const int upto = sh.pick + 1;
+                int left = 0;
+#pragma unroll
+                for (int e = 0; e < 2; ++e) left += 2 * tid + e < upto && list_value(sh, 2 * tid + e) >= cut_m.x;
+                left = block_reduce(left, sh.ints, Add{});
+                draw_from_list(sh, a, mass, r, u, left);
+                return;
+            }
             const unsigned long long at = sh.list[sh.pick];
             cut = Cut{value_of((uint32_t)(at >> 32)), (int)~(uint32_t)at};
         } else {   // more of one value, or nearly, than the list takes
@@ -468,10 +578,7 @@ __global__ __launch_bounds__(kBlock) void token_sample_kernel(TokenSample a)
             cut = find_cut(sh, row, cut, target < whole ? target : whole, [&](float x) { return mass.whole(x); });
         }
     }
-    if (mp > 0.f && mass.c > 0.0) {
-        const Cut c = cut_of_min_p(mass, mp, top, V);
-        if (c.x > cut.x) cut = c;
-    }
+    if (cut_m.x > cut.x) cut = cut_m;
 
     // the draw: the waves' sums, the wave that has the token, the sums of parts of its part
     double mine = 0.0;
@@ -501,7 +608,7 @@ __global__ __launch_bounds__(kBlock) void token_sample_kernel(TokenSample a)
     }
     __syncthreads();
     // its part in kWaves parts of whole loads
-    const int span = (V + kWaves * kStep - 1) / (kWaves * kStep) * kStep;
+    const int span = Row<T>::span_of(V);
     const int steps = (span / kStep + kWaves - 1) / kWaves;
     const int first = holder * span + wv * steps * kStep, stop = (holder + 1) * span;
     auto weights = [&](int s, double (&w)[4], int &i) {
@@ -570,11 +677,8 @@ size_t token_sample_workspace_bytes(int, int, int) { return 16; }
 hipError_t launch_token_sample(const TokenSample &a, bool bf16, hipStream_t stream)
 {
     const dim3 gd((unsigned)a.R), bd(kBlock);
-    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, gd, bd, 0, stream, a); };
-    // as few registers as the row needs
-    const int steps = (a.V + kWaves * kStep - 1) / (kWaves * kStep);
-    if (steps <= 4) bf16 ? launch(token_sample_kernel<uint16_t, 4>) : launch(token_sample_kernel<float, 4>);
-    else bf16 ? launch(token_sample_kernel<uint16_t, 16>) : launch(token_sample_kernel<float, 16>);
+    if (bf16) hipLaunchKernelGGL(token_sample_kernel<uint16_t>, gd, bd, 0, stream, a);
+    else hipLaunchKernelGGL(token_sample_kernel<float>, gd, bd, 0, stream, a);
     return hipGetLastError();
 }
 
