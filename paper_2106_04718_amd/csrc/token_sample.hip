@@ -45,7 +45,6 @@ constexpr int kBins = 2048;   // of a digit of 11 bits, and of top-p's weights
 constexpr int kList = 2048;   // logits that are sorted in LDS
 constexpr int kTopK = 768;    // the list then has some 1500 logits of a smooth distribution
 constexpr int kStep = 4 * kWave;   // logits of a wave's load
-constexpr int kAhead = 4;          // loads on their way
 
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 
@@ -183,6 +182,7 @@ struct Mass {
 
 struct Shared {
     unsigned long long hist[kBins];   // also the sorted list's weights
+    uint32_t hits[kBins];             // logits of each bin
     unsigned long long list[kList];   // key << 32 | ~index: sorted by falling value, then index
     unsigned long long part[kWaves];
     double sum[kWaves];
@@ -217,7 +217,7 @@ struct Row {
         end = V - begin < span ? V : begin + span;
     }
     // f(four logits, index of the first), in the order of the indices; every lane of a wave takes every step
-    template <typename F>
+    template <int kAhead = 4, typename F>
     __device__ __forceinline__ void each4(F f) const {
         const int lane4 = 4 * ((int)threadIdx.x & 63);
         int i = begin;
@@ -230,9 +230,9 @@ struct Row {
         }
         for (; i < end; i += kStep) f(load(i + lane4), i + lane4);
     }
-    template <typename F>
+    template <int kAhead = 4, typename F>
     __device__ __forceinline__ void each(F f) const {
-        each4([&](const f32x4_t &q, int i) {
+        each4<kAhead>([&](const f32x4_t &q, int i) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) f(q[e], i + e);
         });
@@ -446,7 +446,7 @@ __device__ __forceinline__ void draw_from_list(Shared &sh, const TokenSample &a,
 }
 
 template <typename T>
-__global__ __launch_bounds__(kBlock, 8) void token_sample_kernel(TokenSample a)
+__global__ __launch_bounds__(kBlock, 4) void token_sample_kernel(TokenSample a)
 {
     __shared__ Shared sh;
     const int r = blockIdx.x, tid = (int)threadIdx.x, lane = tid & 63, wv = tid / kWave, V = a.V;
@@ -457,7 +457,7 @@ __global__ __launch_bounds__(kBlock, 8) void token_sample_kernel(TokenSample a)
 
     float own = -INFINITY;
     bool bad = false;
-    row.each([&](float x, int) {
+    row.template each<8>([&](float x, int) {
         own = fmaxf(own, x);
         bad |= !(x < INFINITY);
     });
@@ -519,16 +519,26 @@ __global__ __launch_bounds__(kBlock, 8) void token_sample_kernel(TokenSample a)
     }
     if (cut_p) {
         // the weights below 2^-deep, all together, have less than half of 1 - p
-        const double deep = log2((double)V / (1.0 - (double)fmaxf(p, 0.f))) + 1.0, per = kBins / deep;
+        const float deep = (float)(log2((double)V / (1.0 - (double)fmaxf(p, 0.f))) + 1.0);
+        const float per = (float)((double)kBins / (double)deep * mass.c);
+        // 32 bits are enough for the bins: falling with x, and the same in every pass
+        auto bin_of = [&](float x) { return fmaxf((top - x) * per, 0.f); };
         clear_bins(sh);
+        for (int b = tid; b < kBins; b += kBlock) sh.hits[b] = 0;
+        __syncthreads();
         double all = 0.0;
         row.each4([&](const f32x4_t &q, int i) {
+            double w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = cut.keeps(q[e], i + e) ? mass.w(q[e]) : 0.0;   // no branch: four at once
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                if (!cut.keeps(q[e], i + e)) continue;
-                const double y = mass.log2w(q[e]), w = Mass::exp2_of(y), b = -y * per;
-                all += w;
-                if (b < kBins) atomicAdd(&sh.hist[(int)b], mass.whole_of(w));
+                all += w[e];
+                const float b = bin_of(q[e]);
+                if (b < kBins && w[e] > 0.0) {
+                    atomicAdd(&sh.hist[(int)b], mass.whole_of(w[e]));
+                    atomicAdd(&sh.hits[(int)b], 1u);
+                }
             }
         });
         all = block_reduce(all, sh.sum, Add{});
@@ -536,20 +546,19 @@ __global__ __launch_bounds__(kBlock, 8) void token_sample_kernel(TokenSample a)
         const unsigned long long target = t < 1.0 ? 1ull : (unsigned long long)t;
         find_bin<false>(sh, kBins, 0, target);
         const int bin = sh.bin;
-        unsigned long long above = 0;
+        const unsigned long long above = sh.above;
+        int upto = 0;   // logits of the bins 0 .. bin
+#pragma unroll
+        for (int b = 0; b < kBins; b += kBlock) upto += b + tid <= bin ? (int)sh.hits[b + tid] : 0;
+        upto = block_reduce(upto, sh.ints, Add{});
+        const bool whole_nucleus = upto <= kList;
+        const float from = whole_nucleus ? 0.f : (float)bin;
         int n = kList + 1;
-        bool whole_nucleus = false;
-        if (bin >= 0) {
-            above = sh.above;
-            for (int from = 0; from <= bin; from += bin ? bin : 1) {   // bins 0 .. bin, or bin alone
-                n = collect(sh, row, [&](float x, int i) {
-                    const double b = -mass.log2w(x) * per;
-                    return cut.keeps(x, i) && b < (double)(bin + 1) && b >= (double)from;
-                });
-                whole_nucleus = from == 0;
-                if (n <= kList) break;
-            }
-        }
+        if (bin >= 0 && (whole_nucleus || sh.hits[bin] <= kList))
+            n = collect(sh, row, [&](float x, int i) {
+                const float b = bin_of(x);
+                return cut.keeps(x, i) && b >= from && b < (float)(bin + 1);
+            });
         if (n <= kList) {
             sort_list(sh, n);
             unsigned long long w[2];
@@ -587,8 +596,11 @@ __global__ __launch_bounds__(kBlock, 8) void token_sample_kernel(TokenSample a)
 #pragma unroll
         for (int e = 0; e < 4; ++e) kept[e] = cut.keeps(q[e], i + e);
         if (!__any(kept[0] || kept[1] || kept[2] || kept[3])) return;
+        double w[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) mine += kept[e] ? mass.w(q[e]) : 0.0;
+        for (int e = 0; e < 4; ++e) w[e] = mass.w(q[e]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) mine += kept[e] ? w[e] : 0.0;
     });
     mine = wave_reduce(mine, Add{});
     __syncthreads();
