@@ -182,7 +182,7 @@ def test_row_strides_and_alignment(dtype, shift):
 
 
 def test_reused_workspace_and_repeated_calls():
-    ws = api.new_workspace(max(api.token_sample_workspace_bytes(R, V, t) for R, V, t in ((1, 131072, F32), (40, 9001, BF16))), device())
+    ws = api.new_workspace(max(api.token_sample_workspace_bytes(R, V, t) for R, V, t in ((1, 131072, F32), (40, 9001, BF16), (2, 60000, F32))), device())
     cases = [(logits(14, 1, 131072), dict(top_p=0.9)), (logits(15, 40, 9001, dtype=BF16), dict(top_k=50)),
              (logits(16, 1, 131072), {}), (logits(17, 2, 60000), dict(top_k=30))]
     for rep in range(3):
