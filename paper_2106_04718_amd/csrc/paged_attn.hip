@@ -22,8 +22,8 @@
 // would cost as much precision as the rounding of the result.
 //
 // Division of the work.  The positions of all rows are cut into chunks of c units
-// of 128 (4 waves), c such that about kTasks workgroups have one each: lengths
-// are known on the device alone, so every workgroup adds them up and finds its
+// of 128 (4 waves), c such that as many workgroups as fit the chip, or a few times as
+// many, have one each: lengths are known on the device alone, so every workgroup adds them up and finds its
 // own chunk (up to kScanRows rows; above, a kernel before this one does it for
 // all).  Few rows are thus spread over the chip, and a long row among short ones
 // is no one workgroup's.  A row that is one chunk is written at once.  The chunks
@@ -32,6 +32,8 @@
 // square root of their number first.
 #include <math.h>
 #include <stdint.h>
+
+#include <type_traits>
 
 #include "div.h"
 #include "launch.h"
@@ -45,8 +47,8 @@ constexpr int kBlock = kWave * kWaves;
 constexpr int kTile = 32;               // positions a wave attends at a time
 constexpr int kUnit = kTile * kWaves;   // positions a workgroup attends at a time
 constexpr int kHeads = 16;              // query heads of a workgroup
-constexpr int kTaskBits = 10;
-constexpr int kTasks = 1 << kTaskBits;  // chunks aimed at: four for each of the 256 CUs
+constexpr int kPlaces = 512;            // workgroups that fit the 256 CUs at once
+constexpr int kTasks = 4 * kPlaces;     // chunks at most, but for one begun per row
 constexpr int kJoin = 64;               // states joined at a time
 constexpr int kScanRows = 256;          // rows whose lengths every workgroup looks at: four a lane
 
@@ -81,17 +83,36 @@ __device__ __forceinline__ int clamp_len(const PagedAttn &a, int L) {
 }
 
 // Units per chunk for a total of `units` (of all rows; each is attended by ht
-// workgroups): at most kTasks chunks but for one beginning per row.
-__device__ __forceinline__ int chunk_units(unsigned long long units, int ht) {
-    const unsigned long long c = (units * ht + kTasks - 1) >> kTaskBits;
+// workgroups).  As many chunks as workgroups fit the CUs at once; where that makes
+// them long, two or four times as many, so that they end together (64 ragged rows of
+// 2000 positions: 110 us with chunks of 9 units, 121 with 17).  Where they are short,
+// `spare` of the places are left to the chunks that the rows' ends add: a few of them
+// would run after all others (40 rows, 16 heads a key-value head: 83 us, not 94).
+__device__ __forceinline__ int chunk_units(unsigned long long units, int ht, int spare) {
+    const unsigned long long all = units * ht;
+    unsigned long long c = (all + kPlaces - 1) / kPlaces;
+    if (c > 16) c = (c + 1) / 2;
+    else if (spare) c = (all + kPlaces - spare - 1) / (kPlaces - spare);
+    if (c > 24) c = (c + 1) / 2;
     return c < 1 ? 1 : c > (1 << 24) ? 1 << 24 : (int)c;
 }
+__device__ __forceinline__ int spare_places(int R, int ht) { return R * ht / 2 < kPlaces / 4 ? R * ht / 2 : kPlaces / 4; }
 
-__device__ __forceinline__ int wave_sum(int x) {
-#pragma unroll
-    for (int m = 1; m < kWave; m *= 2) x += __shfl_xor(x, m);
-    return x;
+// Inclusive sums over the lanes: of the row of 16 from 1, 2, 4 and 8 lanes before,
+// then the last of a row to the rows behind it.
+template <int CTRL, int ROWS = 0xF>
+__device__ __forceinline__ int dpp(int x) {
+    return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xF, ROWS == 0xF);
 }
+__device__ __forceinline__ int wave_scan(int x) {
+    x += dpp<0x111>(x);
+    x += dpp<0x112>(x);
+    x += dpp<0x114>(x);
+    x += dpp<0x118>(x);
+    x += dpp<0x142, 0xA>(x);
+    return x + dpp<0x143, 0xC>(x);
+}
+__device__ __forceinline__ int wave_sum(int x) { return __builtin_amdgcn_readlane(wave_scan(x), 63); }
 
 // The t-th chunk of up to kScanRows rows; false: there are fewer.
 __device__ __forceinline__ bool find_task(const PagedAttn &a, int ht, int t, Task &out) {
@@ -107,7 +128,11 @@ __device__ __forceinline__ bool find_task(const PagedAttn &a, int ht, int t, Tas
     for (int i = 0; i < 4; ++i) lo += u[i] & 0xffff, hi += u[i] >> 16;
     lo = wave_sum(lo);
     hi = wave_sum(hi);
-    const int c = chunk_units(((unsigned long long)hi << 16) + (unsigned)lo, ht);
+    const unsigned long long units = ((unsigned long long)hi << 16) + (unsigned)lo;
+    int c = chunk_units(units, ht, 0), count = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) count += (u[i] + c - 1) / c;
+    if ((long long)wave_sum(count) * ht > kPlaces) c = chunk_units(units, ht, spare_places(a.R, ht));
     int chunks = 0, split_chunks = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -115,12 +140,7 @@ __device__ __forceinline__ bool find_task(const PagedAttn &a, int ht, int t, Tas
         chunks += s[i];
         split_chunks += s[i] > 1 ? s[i] : 0;
     }
-    int all = chunks, slots = split_chunks;   // inclusive sums over the lanes
-#pragma unroll
-    for (int m = 1; m < kWave; m *= 2) {
-        const int x = __shfl_up(all, m), y = __shfl_up(slots, m);
-        if (lane >= m) all += x, slots += y;
-    }
+    const int all = wave_scan(chunks), slots = wave_scan(split_chunks);
     const unsigned long long past = __ballot(all > t);
     if (past == 0) return false;
     int at = all - chunks, slot = slots - split_chunks, row = 4 * lane, n = 1, first = at;
@@ -151,15 +171,11 @@ __global__ __launch_bounds__(1024) void paged_plan_kernel(PagedAttn a, int ht, i
     for (int r = tid; r < a.R; r += 1024) mine += units_of(clamp_len(a, a.kv_len[r]));
     atomicAdd(&total, mine);
     __syncthreads();
-    const int c = chunk_units(total, ht);
+    const int c = chunk_units(total, ht, spare_places(a.R, ht));
     for (int r0 = 0; r0 < a.R; r0 += 1024) {
         const int r = r0 + tid;
         const int s = r < a.R ? (units_of(clamp_len(a, a.kv_len[r])) + c - 1) / c : 0, m = s > 1 ? s : 0;
-        int x = s, y = m;
-        for (int d = 1; d < kWave; d *= 2) {
-            const int p = __shfl_up(x, d), q = __shfl_up(y, d);
-            if (lane >= d) x += p, y += q;
-        }
+        const int x = wave_scan(s), y = wave_scan(m);
         if (lane == 63) part[0][w] = x, part[1][w] = y;
         __syncthreads();
         int t = base[0] + x - s, slot = base[1] + y - m;
@@ -199,12 +215,17 @@ __device__ __forceinline__ float col_sum(float x) {
     return a + b;
 }
 
-__device__ __forceinline__ u32x4_t load16(const unsigned char *p) {
-    return __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(p));
+// Each byte is read once a call.  A cache that the last level (256 MB) does not keep
+// until the next call is streamed past it, a small one may stay there (us, streamed and
+// not: 2 GB 342 and 364, 787 MB 128 and 142, 235 MB 52 and 56; 50 MB 18.2 and 16.3).
+template <bool STREAM, typename V>
+__device__ __forceinline__ V load(const V *p) {
+    return STREAM ? __builtin_nontemporal_load(p) : *p;
 }
+constexpr long long kStays = 128ll << 20;
 
 // Operands of one tile.  kVe elements of a value row per lane.
-template <int D, bool BF16>
+template <int D, bool BF16, bool STREAM>
 struct Tile {
     static constexpr int kVe = D / 16;
     static constexpr int kSteps = BF16 ? (D + 31) / 32 : D / 16;   // 16-byte loads of a key row per lane
@@ -220,25 +241,25 @@ struct Tile {
     // row: the lane's key row
     __device__ __forceinline__ void load_k(int kb, const unsigned char *row, int g) {
         if constexpr (BF16 && D == 16) {   // the upper half meets zeros of the queries: it has to be finite
-            k[kb][0] = load16(row + 16 * (g & 1));
+            k[kb][0] = load<STREAM>(reinterpret_cast<const u32x4_t *>(row) + (g & 1));
             if (g >= 2) k[kb][0] = u32x4_t{0u, 0u, 0u, 0u};
         } else {
 #pragma unroll
-            for (int s = 0; s < kSteps; ++s) k[kb][s] = load16(row + 64 * s + 16 * g);
+            for (int s = 0; s < kSteps; ++s) k[kb][s] = load<STREAM>(reinterpret_cast<const u32x4_t *>(row) + 4 * s + g);
         }
     }
     __device__ __forceinline__ void load_v(int j, const unsigned char *row, int n) {
         if constexpr (kVw == 0) {
-            v[j][0] = __builtin_nontemporal_load(reinterpret_cast<const uint16_t *>(row) + n);
+            v[j][0] = load<STREAM>(reinterpret_cast<const uint16_t *>(row) + n);
         } else if constexpr (kVw == 1) {
-            v[j][0] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t *>(row) + n);
+            v[j][0] = load<STREAM>(reinterpret_cast<const uint32_t *>(row) + n);
         } else if constexpr (kVw == 2) {
-            const auto x = __builtin_nontemporal_load(reinterpret_cast<const unsigned long long *>(row) + n);
+            const auto x = load<STREAM>(reinterpret_cast<const unsigned long long *>(row) + n);
             v[j][0] = (uint32_t)x, v[j][1] = (uint32_t)(x >> 32);
         } else {
 #pragma unroll
             for (int c = 0; c < kVw / 4; ++c) {
-                const u32x4_t x = load16(row + 256 * c + 16 * n);
+                const u32x4_t x = load<STREAM>(reinterpret_cast<const u32x4_t *>(row) + 16 * c + n);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) v[j][4 * c + i] = x[i];
             }
@@ -323,10 +344,14 @@ __device__ __forceinline__ void join(Load load, float &o, float &m, float &l) {
     }
 }
 
+// Three where the registers allow it (GPT2-shaped, D = 64: 52 us, with two 56).
 template <int D, bool BF16>
-__global__ __launch_bounds__(kBlock, 2) void paged_attn_kernel(PagedAttn a, Geo geo)
+constexpr int kWavesPerSimd = BF16 && D <= 64 ? 3 : 2;
+
+template <int D, bool BF16, bool STREAM>
+__global__ __launch_bounds__(kBlock, (kWavesPerSimd<D, BF16>)) void paged_attn_kernel(PagedAttn a, Geo geo)
 {
-    using T = Tile<D, BF16>;
+    using T = Tile<D, BF16, STREAM>;
     constexpr int kEsize = BF16 ? 2 : 4, kPad = D + 4;
     constexpr bool kHalf = BF16 && D == 16;   // a row is half of what an instruction contracts
     __shared__ __align__(16) float so[kWaves][kHeads][kPad];
@@ -627,11 +652,18 @@ hipError_t launch_paged_attn(const PagedAttn &a, int D, bool bf16, hipStream_t s
     }
     const dim3 gd((unsigned)y.grid), bd(kBlock);
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, gd, bd, 0, stream, a, geo); };
+    const PagedCache &c = a.cache;
+    const bool stream_past = 2ll * c.pages * c.page * a.Hkv * D * (bf16 ? 2 : 4) > kStays;
+    auto of_width = [&](auto width) {
+        constexpr int W = decltype(width)::value;
+        if (bf16) stream_past ? launch(paged_attn_kernel<W, true, true>) : launch(paged_attn_kernel<W, true, false>);
+        else stream_past ? launch(paged_attn_kernel<W, false, true>) : launch(paged_attn_kernel<W, false, false>);
+    };
     switch (D) {
-    case 16: bf16 ? launch(paged_attn_kernel<16, true>) : launch(paged_attn_kernel<16, false>); break;
-    case 32: bf16 ? launch(paged_attn_kernel<32, true>) : launch(paged_attn_kernel<32, false>); break;
-    case 64: bf16 ? launch(paged_attn_kernel<64, true>) : launch(paged_attn_kernel<64, false>); break;
-    default: bf16 ? launch(paged_attn_kernel<128, true>) : launch(paged_attn_kernel<128, false>); break;
+    case 16: of_width(std::integral_constant<int, 16>{}); break;
+    case 32: of_width(std::integral_constant<int, 32>{}); break;
+    case 64: of_width(std::integral_constant<int, 64>{}); break;
+    default: of_width(std::integral_constant<int, 128>{}); break;
     }
     return hipGetLastError();
 }
