@@ -784,6 +784,8 @@ int fs_paged_append(void *K, void *V, int64_t page_stride, int64_t head_stride, 
         return fail(FS_ERR_INVALID_ARG, "the strides of k and v must be multiples of 16 bytes");
     const long long new_bytes = extent(N, token_stride, Hkv, khead_stride, 1, 0, D, esize);
     if (new_bytes < 0) return fail(FS_ERR_UNSUPPORTED, "the strides of k and v are too large");
+    if ((long long)Hkv * (D * (int)esize / 16) > (1 << 24))
+        return fail(FS_ERR_UNSUPPORTED, "Hkv=%d heads of D=%d are more than 2^28 bytes a token", Hkv, D);
     if ((long long)N * Hkv * (D * (int)esize / 16) > (long long)INT_MAX * 128)
         return fail(FS_ERR_UNSUPPORTED, "too many tokens for one launch (N=%d Hkv=%d D=%d)", N, Hkv, D);
     for (const void *c : {(const void *)K, (const void *)V})

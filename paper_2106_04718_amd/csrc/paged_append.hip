@@ -5,6 +5,7 @@
 // position whose table entry names no page of the cache is not written.
 #include <stdint.h>
 
+#include "div.h"
 #include "launch.h"
 
 namespace fs {
@@ -12,44 +13,65 @@ namespace {
 
 typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
 
-// The slot of position pos of row r, in bytes from the cache's base, or -1.
-__device__ __forceinline__ long long slot_of(const PagedCache &c, int r, int pos) {
-    const int j = pos / c.page;
-    if (pos < 0 || j >= c.cols) return -1;
-    const int pg = c.table[(size_t)r * c.ld_table + j];
-    if (pg < 0 || pg >= c.pages) return -1;
-    return pg * c.page_bytes + (pos - j * c.page) * c.slot_bytes;
-}
-
-// One lane moves 16 bytes of one token's key and value row.
-__global__ __launch_bounds__(256) void paged_append_kernel(PagedCache c, const unsigned char *k, const unsigned char *v,
-                                                           long long token_bytes, long long khead_bytes, int N,
-                                                           const int32_t *start, const int32_t *offsets, int R, int Hkv,
-                                                           int chunks)
+// A workgroup moves the key and value rows of one token after another, kAhead of them
+// at a time: which row a token is of, and where that has it, is the same for all its
+// lanes.  Lane i moves 16 bytes of every token: chunk i of its Hkv * chunks.
+constexpr int kThreads = 256;
+template <int kAhead>
+__global__ __launch_bounds__(kThreads) void paged_append_kernel(PagedCache c, const unsigned char *k, const unsigned char *v,
+                                                                long long token_bytes, long long khead_bytes, int N,
+                                                                const int32_t *start, const int32_t *offsets, int R,
+                                                                int per, Div by_chunks, int chunks, Div by_page)
 {
-    const long long id = (long long)blockIdx.x * 256 + threadIdx.x;
-    const int per = Hkv * chunks;
-    const int n = (int)(id / per);
-    if (n >= N) return;
-    const int h = (int)(id % per) / chunks, ch = (int)(id % per) % chunks;
-    int r = n, i = 0;
-    if (offsets) {   // the last row whose tokens begin at or before n
-        int lo = 0, hi = R;
+    const int n0 = (int)blockIdx.x * kAhead;
+    long long at[kAhead];   // of each token's slot, or -1
+    int lo = 0;
+    if (offsets) {          // the last row whose tokens begin at or before the first token
+        int hi = R;
         while (hi - lo > 1) {
             const int mid = (lo + hi) / 2;
-            (offsets[mid] <= n ? lo : hi) = mid;
+            (offsets[mid] <= n0 ? lo : hi) = mid;
         }
-        if (n < offsets[lo] || n >= offsets[lo + 1]) return;
-        r = lo;
-        i = n - offsets[lo];
     }
-    const long long pos = (long long)start[r] + i;
-    const long long at = pos > 0x7fffffff ? -1 : slot_of(c, r, (int)pos);
-    if (at < 0) return;
-    const size_t from = (size_t)n * token_bytes + (size_t)h * khead_bytes + ch * 16;
-    const size_t to = (size_t)at + (size_t)h * c.head_bytes + ch * 16;
-    *reinterpret_cast<u32x4_t *>(c.K + to) = *reinterpret_cast<const u32x4_t *>(k + from);
-    *reinterpret_cast<u32x4_t *>(c.V + to) = *reinterpret_cast<const u32x4_t *>(v + from);
+#pragma unroll
+    for (int e = 0; e < kAhead; ++e) {
+        const int n = n0 + e;
+        at[e] = -1;
+        if (n >= N) continue;
+        long long pos;
+        if (offsets) {
+            while (lo + 1 < R && offsets[lo + 1] <= n) ++lo;
+            if (n < offsets[lo] || n >= offsets[lo + 1]) continue;
+            pos = (long long)start[lo] + (n - offsets[lo]);
+        } else {
+            lo = n;
+            pos = start[n];
+        }
+        if (pos < 0 || pos > 0x7fffffff) continue;
+        const int j = (int)by_page((unsigned)pos);
+        if (j >= c.cols) continue;
+        const int pg = c.table[(size_t)lo * c.ld_table + j];
+        if (pg >= 0 && pg < c.pages) at[e] = pg * c.page_bytes + ((int)pos - j * c.page) * c.slot_bytes;
+    }
+    for (int i = threadIdx.x; i < per; i += kThreads) {
+        const int h = (int)by_chunks((unsigned)i), ch = i - h * chunks;
+        const size_t from = (size_t)n0 * token_bytes + (size_t)h * khead_bytes + (size_t)ch * 16;
+        const size_t to = (size_t)h * c.head_bytes + (size_t)ch * 16;
+        u32x4_t x[kAhead], y[kAhead];
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e) {
+            // a token that goes nowhere reads the first one's row
+            const size_t f = from + (at[e] >= 0 ? (size_t)e * token_bytes : 0);
+            x[e] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(k + f));
+            y[e] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(v + f));
+        }
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e) {
+            if (at[e] < 0) continue;
+            *reinterpret_cast<u32x4_t *>(c.K + at[e] + to) = x[e];
+            *reinterpret_cast<u32x4_t *>(c.V + at[e] + to) = y[e];
+        }
+    }
 }
 
 }  // namespace
@@ -59,10 +81,14 @@ hipError_t launch_paged_append(const PagedCache &cache, const void *k, const voi
                                int row_bytes, hipStream_t stream)
 {
     const int chunks = row_bytes / 16;
-    const long long n = (long long)N * Hkv * chunks;
-    hipLaunchKernelGGL(paged_append_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, stream, cache,
-                       static_cast<const unsigned char *>(k), static_cast<const unsigned char *>(v), token_bytes,
-                       khead_bytes, N, start, offsets, R, Hkv, chunks);
+    // a token a workgroup until they fill the chip; then four, whose loads are on their way together
+    auto launch = [&](auto kernel, int ahead) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)((N + (long long)ahead - 1) / ahead)), dim3(kThreads), 0, stream, cache,
+                           static_cast<const unsigned char *>(k), static_cast<const unsigned char *>(v), token_bytes,
+                           khead_bytes, N, start, offsets, R, Hkv * chunks, make_div(chunks), chunks, make_div(cache.page));
+    };
+    if (N <= 2048) launch(paged_append_kernel<1>, 1);
+    else launch(paged_append_kernel<4>, 4);
     return hipGetLastError();
 }
 

@@ -50,7 +50,7 @@ CACHE = [
     (dict(offsets=5 * F + 1), INVALID, "aligned"), (dict(ts=132), INVALID, "multiples of 16"),
     (dict(ks=-64), INVALID, "negative stride"), (dict(k=BIG + 64), INVALID, "overlaps"),
     (dict(table=2 * BIG + 64), INVALID, "overlaps"), (dict(start=BIG), INVALID, "overlaps"),
-    (dict(N=2**31 - 1, Hkv=64, hs=64 * 16, ps=64 * 64 * 16), UNSUPPORTED, "too many tokens"),
+    (dict(Hkv=1 << 22, hs=0), UNSUPPORTED, "heads"), (dict(N=2**31 - 1, Hkv=64, hs=64 * 16, ps=64 * 64 * 16), UNSUPPORTED, "too many tokens"),
 ])
 def test_append_rejects(kw, status, needle):
     assert append(**kw) == status

@@ -96,6 +96,44 @@ def test_every_row_has_its_own_settings():
           min_p=rng.choice([0, 0.1, 1, 2, np.nan, -1], R))
 
 
+@pytest.mark.parametrize("R,V", [(32, 40001), (33, 40001), (7, 32769), (7, 32768), (3, 36864), (2, 36865), (32, 131072)])
+def test_each_row_its_settings_around_the_sizes_where_the_kernels_change(R, V):
+    """Up to 32 rows of more than 32768 logits go through kernels with a workgroup per
+    slice of 4096, others through a workgroup per row."""
+    rng = np.random.default_rng(R + V)
+    x, u = logits(V - R, R, V, dtype=BF16 if V % 2 else F32)
+    if R > 3:
+        x = x.copy()
+        x[1], x[2, V - 1] = (workloads.BF16_NAN if x.dtype == np.uint16 else np.nan), x[2, 0]
+        x[3] = 0                                    # a row of one value: given up by the slices
+        x[0, 4096:] = x[0, 4096]                    # all but a slice equal
+    kw = dict(temperature=rng.choice([0, 0.5, 0.8, 1, 2, -1, np.inf], R), top_k=rng.choice([0, 1, 7, 60, 190, 200, 1500, V], R),
+              top_p=rng.choice([0, 0.3, 0.9, 0.95, 1, 1.5], R), min_p=rng.choice([0, 0, 0.1, 1], R))
+    check(x, u, "mixed", **kw)
+    for off in ("top_k", "top_p", "min_p", "temperature"):
+        check(x, u, f"without {off}", **{n: a for n, a in kw.items() if n != off})
+    check(x, u, "top_p alone", top_p=kw["top_p"])
+    check(x, u, "min_p alone", min_p=kw["min_p"])
+
+
+def test_slices_of_bans_alone_and_few_finite_logits():
+    rng = np.random.default_rng(21)
+    x = np.full((6, 50000), -np.inf, np.float32)
+    for r, n in enumerate((1, 3, 40, 900, 5000, 30000)):
+        x[r, rng.choice(50000, n, replace=False)] = rng.standard_normal(n).astype(np.float32)
+    u = rng.random(6).astype(np.float32)
+    for mode, kw in MODES.items():
+        check(x, u, f"few finite, {mode}", **kw)
+
+
+def test_candidates_of_every_slice_exceed_the_list():
+    """Top-k of 190 over 32 slices: several thousand candidates, bounded once more."""
+    x, u = logits(22, 2, 131072, sd=1.0)
+    for k in (150, 190, 192, 193):
+        check(x, u, f"k={k}", top_k=k)
+        check(x, u, f"k={k}", top_k=k, top_p=0.8, min_p=0.02)
+
+
 def test_many_rows():
     x, u = logits(5, 3000, 77)
     check(x, u, "3000 rows", top_k=9, top_p=0.9)
