@@ -566,11 +566,13 @@ size_t fs_paged_attn_workspace_bytes(int R, int Hq, int Hkv, int page, int cols,
  * over the positions whose pg(j) lies in [0, P); out[r,h,:] = 0 where there is
  * none.  Positions j >= L are never read.
  *
- * With k and v (both or neither) position L - 1 is the token itself: its key
- * and value are taken from k[r,g,:] and v[r,g,:] and also written to the cache
- * (fs_paged_append's rule; a row of L == 0 or without that page writes nothing
- * and does not attend it).  kv_len counts the new token.  A page that several
- * rows' tables share must not be the one that a row writes.
+ * With k and v (both or neither) position kv_len[r] - 1 is the token itself: its
+ * key and value are taken from k[r,g,:] and v[r,g,:] and also written to the
+ * cache.  kv_len counts the new token.  fs_paged_append's rule holds: a token
+ * with no slot (kv_len[r] outside [1, cols * page], or no page there) is neither
+ * written nor attended.  A page that several rows' tables share must not be the
+ * one that a row writes.  An infinite value among the attended ones gives an
+ * infinity or NaN.
  *
  * Arguments (device pointers except the sizes; strides in elements):
  *   q            [R, Hq, D] dtype, strides q_row_stride and q_head_stride

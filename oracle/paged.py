@@ -55,7 +55,7 @@ def paged_attn(q, K, V, table, kv_len, k=None, v=None, scale=None):
     for r in range(R):
         L = min(max(int(kv_len[r]), 0), table.shape[1] * page)
         slots = [_slot(table, r, j, page, P) for j in range(L)]
-        if k is not None and L > 0 and slots[-1] is not None:
+        if k is not None and L > 0 and int(kv_len[r]) == L and slots[-1] is not None:
             K[slots[-1][0], :, slots[-1][1]] = k[r]
             V[slots[-1][0], :, slots[-1][1]] = v[r]
         slots = [s for s in slots if s is not None]

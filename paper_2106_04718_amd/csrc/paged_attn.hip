@@ -373,7 +373,7 @@ __global__ __launch_bounds__(kBlock, (kWavesPerSimd<D, BF16>)) void paged_attn_k
     }
     const int qt = (int)geo.by_hkv(ht), h = ht - qt * a.Hkv;
     const int heads = geo.G - qt * kHeads < kHeads ? geo.G - qt * kHeads : kHeads;
-    const int r = task.r, L = clamp_len(a, a.kv_len[r]);
+    const int r = task.r, given = a.kv_len[r], L = clamp_len(a, given);
     const int begin = task.split * task.c * kUnit;   // below 2^31: a unit of the row's
     const int end = L - begin < task.c * (long long)kUnit ? L : begin + task.c * kUnit;
 
@@ -393,7 +393,7 @@ __global__ __launch_bounds__(kBlock, (kWavesPerSimd<D, BF16>)) void paged_attn_k
     const unsigned char *Kh = c.K + (size_t)h * c.head_bytes, *Vh = c.V + (size_t)h * c.head_bytes;
     const int32_t *table = c.table + (size_t)r * c.ld_table;
     const size_t fresh_off = (size_t)r * a.new_row_bytes + (size_t)h * a.new_head_bytes;
-    const int fresh = a.k ? L - 1 : -1;
+    const int fresh = a.k && given == L ? L - 1 : -1;   // a row past its table has no place for the token
 
     // Pages: lane l looks up position t0 + l % 32 of a tile, two tiles ahead of
     // its use; `off` is the position's slot in units of 16 bytes and `live` the

@@ -178,6 +178,27 @@ def test_new_token_without_a_page_writes_nothing():
     check(d, "no page for the new token")
 
 
+def test_a_full_row_has_no_place_for_a_new_token():
+    """kv_len past the table: the cached positions are attended as they are."""
+    d = make(41, [64, 64, 30], 4, 2, 64, 16, BF16, new=True)
+    rng = np.random.default_rng(41)
+    for x in ("K", "V"):
+        d[x] = np.where(d[x] == workloads.BF16_NAN, draw(rng, d[x].shape, BF16), d[x])
+    d["kv_len"] = np.array([65, 64, 2**31 - 1], np.int32)
+    check(d, "full rows")
+
+
+def test_debug_mode_rejects_lengths_outside_the_table():
+    d = make(42, [20, 64], 4, 2, 64, 16, BF16)
+    t = {x: dev_of(d[x]) for x in d}
+    call = lambda n: api.paged_attn(t["q"], t["K"], t["V"], t["table"], torch.tensor(n, dtype=torch.int32, device=device()))
+    with api.validate_lengths():
+        call([20, 64])
+        for bad in ([20, 65], [-1, 64]):
+            with pytest.raises(N.NativeError, match="kv_len"):
+                call(bad)
+
+
 def test_large_scores_and_one_key_that_takes_all():
     d = make(15, [400, 77], 4, 2, 64, 16, F32, sigma=20.0)
     check(d, "scores of hundreds")
