@@ -15,7 +15,9 @@ typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
 
 // A workgroup moves the key and value rows of one token after another, kAhead of them
 // at a time: which row a token is of, and where that has it, is the same for all its
-// lanes.  Lane i moves 16 bytes of every token: chunk i of its Hkv * chunks.
+// lanes.  Lane i moves 16 bytes of every token: chunk i of its Hkv * chunks.  Bound by
+// HBM: 48000 tokens of 4 KB, 393 MB in and out, 81 us, 4.9 TB/s (97 with a lane per 16
+// bytes that finds its own row).
 constexpr int kThreads = 256;
 template <int kAhead>
 __global__ __launch_bounds__(kThreads) void paged_append_kernel(PagedCache c, const unsigned char *k, const unsigned char *v,

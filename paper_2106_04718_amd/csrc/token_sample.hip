@@ -12,8 +12,9 @@
 // of the kept w exceeds u times their total.
 //
 // A draw next to a border of two tokens depends on the sums, and a large
-// vocabulary has many borders: with the weights in 32 bits one draw in some ten
-// thousand would be another token's.  Weights and sums are 64-bit.
+// vocabulary has many borders: with weights and sums in 32 bits 7 draws in 1000 would
+// be another token's, with the weights alone in 32 bits 1 in 100000 (4 million draws
+// from rows of 50257 normal logits of deviation 1.5).  Weights and sums are 64-bit.
 //
 // No pass sorts or scans the row:
 //   top-k      The k-th largest of the threads' 1024 maxima is a bound that at
@@ -35,7 +36,7 @@
 //                  passes, which run once a row: waiting for their instructions cost
 //                  more than reading again).  For many rows, and for the rows that
 //                  the other way gives up.
-//   four kernels   with a workgroup per slice of 4096 or 16384 logits, for up to
+//   four kernels   with a workgroup per slice of 4096 logits, for up to
 //                  kSliceRows rows of more than kSliceFrom logits:
 //     slice_kernel   reads the logits.  Its maximum, and what goes by it alone:
 //                    greedy's token, top-k's candidates of the slice, the sum of the
@@ -48,6 +49,10 @@
 //                    draw.  sample_row for rows given up.
 //                  One row of 131072 then is on 32 CUs, and the bins' atomic
 //                  additions, which are what a CU's LDS is slowest at, with it.
+//
+// Measured: 128 rows of 50264 with top-k and top-p 17.4 us, 512 bf16 rows of 50257
+// without a filter 44, 256 rows of 151936 with settings of their own 153, one row of
+// 131072 with top-p 33.
 #include <math.h>
 #include <stdint.h>
 
