@@ -107,3 +107,18 @@ def test_frequencies_are_the_kept_probabilities(kw):
     # a token of probability 1/20000 or more spans one of the 20000 midpoints at
     # least, so each token that was never drawn has less than that
     assert -1e-9 <= 1 - p.sum() <= np.count_nonzero(p == 0) / 20000 + 1e-9
+
+
+def test_a_token_past_its_rows_table_is_neither_written_nor_attended():
+    """A row of two positions, both held: a new token at length 3 has no place, at
+    length 2 it is the second."""
+    K = np.arange(4, dtype=np.float32).reshape(1, 1, 2, 2)
+    V = K + 10
+    q, table = np.zeros((1, 1, 2), np.float32), np.zeros((1, 1), np.int32)
+    k, v = np.full((1, 1, 2), 50, np.float32), np.full((1, 1, 2), 70, np.float32)
+    out, K3, V3 = paged.paged_attn(q, K, V, table, [3], k, v)
+    assert (K3 == K).all() and (V3 == V).all()
+    np.testing.assert_array_equal(out[0, 0], [11, 12])   # the mean of [10, 11] and [12, 13]
+    out, K2, V2 = paged.paged_attn(q, K, V, table, [2], k, v)
+    assert (K2[0, 0, 1] == 50).all() and (V2[0, 0, 1] == 70).all()
+    np.testing.assert_array_equal(out[0, 0], [40, 40.5])
