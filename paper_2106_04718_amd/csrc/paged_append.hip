@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include "div.h"
+#include "grid.h"
 #include "launch.h"
 
 namespace fs {
@@ -25,7 +26,9 @@ __global__ __launch_bounds__(kThreads) void paged_append_kernel(PagedCache c, co
                                                                 const int32_t *start, const int32_t *offsets, int R,
                                                                 int per, Div by_chunks, int chunks, Div by_page)
 {
-    const int n0 = (int)blockIdx.x * kAhead;
+    const unsigned first = wide_index() * kAhead;
+    if (first >= (unsigned)N) return;
+    const int n0 = (int)first;
     long long at[kAhead];   // of each token's slot, or -1
     int lo = 0;
     if (offsets) {          // the last row whose tokens begin at or before the first token
@@ -85,7 +88,7 @@ hipError_t launch_paged_append(const PagedCache &cache, const void *k, const voi
     const int chunks = row_bytes / 16;
     // a token a workgroup until they fill the chip; then four, whose loads are on their way together
     auto launch = [&](auto kernel, int ahead) {
-        hipLaunchKernelGGL(kernel, dim3((unsigned)((N + (long long)ahead - 1) / ahead)), dim3(kThreads), 0, stream, cache,
+        hipLaunchKernelGGL(kernel, wide_grid((N + (long long)ahead - 1) / ahead), dim3(kThreads), 0, stream, cache,
                            static_cast<const unsigned char *>(k), static_cast<const unsigned char *>(v), token_bytes,
                            khead_bytes, N, start, offsets, R, Hkv * chunks, make_div(chunks), chunks, make_div(cache.page));
     };
