@@ -36,6 +36,7 @@
 #include <type_traits>
 
 #include "div.h"
+#include "grid.h"
 #include "launch.h"
 
 namespace fs {
@@ -362,7 +363,8 @@ __global__ __launch_bounds__(kBlock, (kWavesPerSimd<D, BF16>)) void paged_attn_k
 
     const int lane = (int)threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
     const int n = lane & 15, g = lane >> 4;
-    const int t = (int)geo.by_ht(blockIdx.x), ht = (int)blockIdx.x - t * geo.ht;
+    const unsigned wg = wide_index();
+    const int t = (int)geo.by_ht(wg), ht = (int)wg - t * geo.ht;
     Task task;
     if (geo.tasks) {
         const int4 head = geo.tasks[0];
@@ -651,7 +653,7 @@ hipError_t launch_paged_attn(const PagedAttn &a, int D, bool bf16, hipStream_t s
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    const dim3 gd((unsigned)y.grid), bd(kBlock);
+    const dim3 gd = wide_grid(y.grid), bd(kBlock);
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, gd, bd, 0, stream, a, geo); };
     const PagedCache &c = a.cache;
     const bool stream_past = 2ll * c.pages * c.page * a.Hkv * D * (bf16 ? 2 : 4) > kStays;

@@ -43,3 +43,20 @@ def test_append_of_more_tokens_than_one_dimension_holds(offsets):
         same = torch.equal(C.view(-1, D)[:N], x.view(N, D))
         assert same, "not every token is in its slot"
         assert not C.view(-1, D)[N:].any()
+
+
+@pytest.mark.parametrize("R", [(1 << 24) - 1000, 1 << 24])
+def test_attention_of_more_rows_than_one_dimension_holds(R):
+    """Rows of one position: each result is that position's value, bit for bit.  Up to
+    a few thousand workgroups more than rows are launched."""
+    say(f"[paged grid] attention of {R} rows")
+    dev, P, page, D = device(), 512, 256, 16
+    q, K, V = noise(R, 1, D), noise(P, 1, page, D), noise(P, 1, page, D)
+    r = torch.arange(R, device=dev)
+    table, kv_len = (r % P).int()[:, None], (r % 3 != 1).int()
+    out = torch.full((R, 1, D), -1.0, dtype=BF16, device=dev)
+    api.paged_attn(q, K, V, table, kv_len, out=out)
+    torch.cuda.synchronize()
+    want = V[(r % P), :, 0] * kv_len[:, None, None].to(BF16)
+    same = torch.equal(out, want)   # -0.0 of a masked row equals 0
+    assert same, "not every row is attended"
