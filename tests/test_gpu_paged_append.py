@@ -1,5 +1,6 @@
-"""paged_append of many tokens, which go four at a time, compared bit for bit with an
-indexed assignment."""
+"""paged_append where its kernels change: tokens of few bytes stand side by side in
+a workgroup (up to 64 chunks of 16 bytes each), many tokens go four at a time.
+Compared bit for bit with an indexed assignment, at sizes around both rules."""
 import numpy as np
 import pytest
 import torch
@@ -10,7 +11,7 @@ from _gpu import device, say
 
 pytestmark = pytest.mark.gpu
 
-BF16 = torch.bfloat16
+BF16, F32 = torch.bfloat16, torch.float32
 
 
 def check(lens, Hkv, D, page, dtype, lead=0, trail=0, seed=0, bad=()):
@@ -45,6 +46,21 @@ def check(lens, Hkv, D, page, dtype, lead=0, trail=0, seed=0, bad=()):
     torch.cuda.synchronize()
     same = torch.equal(K, wK) and torch.equal(V, wV)
     assert same, f"R={R} N={N} Hkv={Hkv} D={D}"
+
+
+# chunks of a token: 2, 6, 40, 56, 64 side by side; 72, 128 and 320 one behind another
+@pytest.mark.parametrize("Hkv,D,dtype", [(1, 16, BF16), (3, 16, BF16), (5, 64, BF16), (7, 32, F32), (4, 128, BF16),
+                                         (9, 64, BF16), (8, 128, BF16), (10, 128, F32)])
+@pytest.mark.parametrize("turns", [0.4, 1, 1.1])
+def test_around_the_number_of_tokens_that_go_four_at_a_time(Hkv, D, dtype, turns):
+    per = Hkv * D * (2 if dtype == BF16 else 4) // 16
+    side = 256 // per if per <= 64 else 1
+    n = int(2048 * side * turns)
+    parts = np.array([1, 0, 3, 700, 5, 0, 0, 1000, 2, 333])
+    lens = parts * n // parts.sum()
+    lens[3] += n - 7 - lens.sum()
+    check(lens, Hkv, D, 16, dtype, lead=3, trail=4, seed=per, bad=[4])        # n tokens, seven of no row
+    check(lens, Hkv, D, 7, dtype, seed=per + 1)
 
 
 @pytest.mark.parametrize("Hkv,D", [(1, 16), (2, 64), (8, 128)])
