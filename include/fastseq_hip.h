@@ -589,9 +589,8 @@ size_t fs_paged_attn_workspace_bytes(int R, int Hq, int Hkv, int page, int cols,
  *                other, eagerly or replayed from graphs.
  *   stream       hipStream_t (NULL = default stream)
  * Supported: fs_paged_append's set; Hq a multiple of Hkv, R * Hq <= 2^24.
- * Arithmetic: products and sums in fp32 (bf16 weights are taken as a sum of
- * two bf16 values), one rounding at the end.  The bits depend on the data and
- * the sizes, never on run or launch.
+ * Arithmetic: weights, products and sums in fp32, one rounding at the end.  The
+ * bits depend on the data and the sizes, never on run or launch.
  * Errors: those of fs_paged_append; FS_ERR_INVALID_ARG also for Hq not a
  * multiple of Hkv, one of k and v without the other, a scale that is not
  * finite, a workspace that is too small or misaligned, or out or the workspace
