@@ -218,9 +218,12 @@ __device__ __forceinline__ float col_sum(float x) {
     return a + b;
 }
 
-// Each byte is read once a call.  A cache that the last level (256 MB) does not keep
-// until the next call is streamed past it, a small one may stay there (us, streamed and
-// not: 2 GB 342 and 364, 787 MB 128 and 142, 235 MB 52 and 56; 50 MB 18.2 and 16.3).
+// Up to kHeads query heads on a key-value head, each byte is read once a call.  A cache
+// that the last level (256 MB) does not keep until the next call is then streamed past
+// it, a small one may stay there (us, streamed and not: 2 GB 342 and 364, 787 MB 128 and
+// 142, 235 MB 52 and 56; 50 MB 18.2 and 16.3).  More heads are of several workgroups,
+// which read the same bytes: never streamed (64 heads on one, 393 MB: 310 and 243; 32 on
+// each of two, 197 MB: 93 and 77; 24 on each of eight, 787 MB: 316 and 248).
 template <bool STREAM, typename V>
 __device__ __forceinline__ V load(const V *p) {
     return STREAM ? __builtin_nontemporal_load(p) : *p;
@@ -671,7 +674,7 @@ hipError_t launch_paged_attn(const PagedAttn &a, int D, bool bf16, hipStream_t s
     const dim3 gd = wide_grid(y.grid), bd(kBlock);
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, gd, bd, 0, stream, a, geo); };
     const PagedCache &c = a.cache;
-    const bool stream_past = 2ll * c.pages * c.page * a.Hkv * D * (bf16 ? 2 : 4) > kStays;
+    const bool stream_past = y.G <= kHeads && 2ll * c.pages * c.page * a.Hkv * D * (bf16 ? 2 : 4) > kStays;
     auto of_width = [&](auto width) {
         constexpr int W = decltype(width)::value;
         if (bf16) stream_past ? launch(paged_attn_kernel<W, true, true>) : launch(paged_attn_kernel<W, true, false>);
