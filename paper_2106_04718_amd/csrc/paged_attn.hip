@@ -50,7 +50,7 @@ constexpr int kBlock = kWave * kWaves;
 constexpr int kTile = 32;               // positions a wave attends at a time
 constexpr int kUnit = kTile * kWaves;   // positions a workgroup attends at a time
 constexpr int kHeads = 16;              // query heads of a workgroup
-constexpr int kPlaces = 512;            // workgroups that fit the 256 CUs at once
+constexpr int kPlaces = 512;            // workgroups that fit the 256 CUs at once, two each (some kernels three)
 constexpr int kTasks = 4 * kPlaces;     // chunks at most, but for one begun per row
 constexpr int kJoin = 64;               // states joined at a time
 constexpr int kScanRows = 256;          // rows whose lengths every workgroup looks at: four a lane
@@ -90,12 +90,14 @@ __device__ __forceinline__ int clamp_len(const PagedAttn &a, int L) {
 // them long, two or four times as many, so that they end together (64 ragged rows of
 // 2000 positions: 110 us with chunks of 9 units, 121 with 17).  Where they are short,
 // `spare` of the places are left to the chunks that the rows' ends add: a few of them
-// would run after all others (40 rows, 16 heads a key-value head: 83 us, not 94).
+// would run after all others (40 rows, 16 heads a key-value head: 83 us, not 94).  That
+// may make them long again (us as they are and halved: 19 units 92 and 97, 20 units 100 and
+// 103; 21 and 22 units 103 and 105, 109 and 102, 98 and 94, 104 and 100).
 __device__ __forceinline__ int chunk_units(unsigned long long units, int ht, int spare) {
     const unsigned long long all = units * ht;
     unsigned long long c = (all + kPlaces - 1) / kPlaces;
     if (c > 16) c = (c + 1) / 2;
-    else if (spare) c = (all + kPlaces - spare - 1) / (kPlaces - spare);
+    else if (spare && (c = (all + kPlaces - spare - 1) / (kPlaces - spare)) > 20) c = (c + 1) / 2;
     if (c > 24) c = (c + 1) / 2;
     return c < 1 ? 1 : c > (1 << 24) ? 1 << 24 : (int)c;
 }
@@ -163,7 +165,9 @@ __device__ __forceinline__ bool find_task(const PagedAttn &a, int ht, int t, Tas
 }
 
 // The chunks of any number of rows, by one workgroup: tasks[1 + t] = (row,
-// split, splits, slot), tasks[0] = (number of chunks, units per chunk).
+// split, splits, slot), tasks[0] = (number of chunks, units per chunk).  It costs 2.4 us
+// where the rows are short (256 and 257 of up to 64 positions: 9.0 and 11.4), 6 where they
+// are cut (of up to 1000 positions, 530 MB: 95 and 101).
 __global__ __launch_bounds__(1024) void paged_plan_kernel(PagedAttn a, int ht, int4 *tasks) {
     __shared__ unsigned long long total;
     __shared__ int part[2][16], base[2];
@@ -174,6 +178,7 @@ __global__ __launch_bounds__(1024) void paged_plan_kernel(PagedAttn a, int ht, i
     for (int r = tid; r < a.R; r += 1024) mine += units_of(clamp_len(a, a.kv_len[r]));
     atomicAdd(&total, mine);
     __syncthreads();
+    // places are left without a look at the chunks' number: rows alone make more than kScanRows of them
     const int c = chunk_units(total, ht, spare_places(a.R, ht));
     for (int r0 = 0; r0 < a.R; r0 += 1024) {
         const int r = r0 + tid;
