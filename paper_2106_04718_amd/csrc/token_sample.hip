@@ -37,7 +37,8 @@
 //                  more than reading again).  For many rows, and for the rows that
 //                  the other way gives up.
 //   four kernels   with a workgroup per slice of 4096 logits, for up to
-//                  kSliceRows rows of more than kSliceFrom logits:
+//                  kSliceRows rows of more than kSliceFrom logits (and, with
+//                  top-k, of small k):
 //     slice_kernel   reads the logits.  Its maximum, and what goes by it alone:
 //                    greedy's token, top-k's candidates of the slice, the sum of the
 //                    weights (of the slice's maximum).
@@ -917,10 +918,19 @@ using B = Block<4>;
 constexpr int kCus = 256;
 // Slices pay for four more launches and for what they hand each other.  Rows of
 // 131072, one / 32 / 128 of them, in slices and by one workgroup each (us): top-p 33,
-// 64, 173 and 101, 102, 113; no filter 18, 19, 30 and 34, 36, 45; top-k 26, 29, 39 and
-// 15, 16, 29.  Rows of 10000: 32, 51, 55 and 22, 29, 30 with top-p.
+// 64, 173 and 101, 102, 113; no filter 18, 19, 30 and 34, 36, 45.  Rows of 10000: 32, 51,
+// 55 and 22, 29, 30 with top-p.
 constexpr int kSliceRows = 32;
 constexpr int kSliceFrom = 32768;
+// Top-k: the slices' candidates grow with k, and a workgroup's time for a row does not.
+// One row of 131072 with k = 8, 48, 64, 192 in slices 15, 23, 27, 77 us; left to a workgroup
+// behind the slices' launches 20, 21, 23, 29; by one at once 16, 17, 18, 25.  (50264: 14, 17, 19,
+// 43; 17, 17, 17, 24; 12, 13, 13, 20.  2^20: 27, 94, 124, 516; 96, 98, 99, 105; 93, 93, 95, 102.)
+// The settings are on the device: there, rows of k above kSliceTopK are left out of the
+// slices.  The host knows which are not given: with top-k and no top-p, rows of up to
+// kSliceFromTopK logits go by a workgroup at once.
+constexpr int kSliceTopK = 48;
+constexpr int kSliceFromTopK = 131072;
 constexpr int kLoads = 4;                              // loads of four logits a thread
 constexpr int kSlice = 4 * kLoads * B::kBlock;         // logits of a slice: 4096
 constexpr int kSlices = 1024;                          // of a row at most
@@ -1072,8 +1082,12 @@ __global__ __launch_bounds__(B::kBlock, 8) void slice_kernel(TokenSample a, Slic
 {
     __shared__ SmallShared sh;
     const int s = (int)z.by_r(blockIdx.x), r = (int)blockIdx.x - s * a.R, tid = (int)threadIdx.x, V = a.V;
-    const Slice<T> row(logits_of<T>(a, r), V, s);
     const Setting st(a, r);
+    if (st.cuts_k(V) && st.k > kSliceTopK && st.temp != 0.f) {   // sample_row's
+        if (tid == 0 && s == 0) z.state[r] = RowState{kGivenUp, kDone, 0, 0.f, 0};
+        return;
+    }
+    const Slice<T> row(logits_of<T>(a, r), V, s);
     float own = -INFINITY;
     bool bad = false;
     row.each([&](float x, int) {
@@ -1110,7 +1124,7 @@ __global__ __launch_bounds__(B::kBlock, 8) void slice_kernel(TokenSample a, Slic
             int at = V;
             row.each([&](float x, int i) { at = x == rec.top && i < at ? i : at; });
             rec.at = B::block_reduce(at, sh.ints, Min{});
-        } else if (st.cuts_k(V) && st.k <= B::kTopK) {
+        } else if (st.cuts_k(V)) {
             const float bound = B::bound_of(sh, own, rec.top, st.k);
             rec.count = B::collect(sh, row, [&](float x, int) { return x > -INFINITY && x >= bound; });
             unsigned long long *to = z.candidate + ((size_t)r * z.S + s) * kCandidates;
@@ -1183,7 +1197,7 @@ __device__ __forceinline__ void merge_top_k(RowShared &sh, const TokenSample &a,
     const int tid = (int)threadIdx.x;
     int *start = reinterpret_cast<int *>(sh.hits);   // of the slices, among all candidates
     int count[kMine], sum = 0;
-    bool given_up = st.k > B::kTopK;
+    bool given_up = false;
 #pragma unroll
     for (int e = 0; e < kMine; ++e) {
         const int s = kMine * tid + e;
@@ -1262,6 +1276,7 @@ __global__ __launch_bounds__(B::kBlock, 4) void merge_kernel(TokenSample a, Slic
     }
     const int r = (int)blockIdx.x;
     const Setting st(a, r);
+    if (z.state[r].kind == kGivenUp) return;
     const SliceRecord *rec = z.record + (size_t)r * z.S;
     const float top = top_of(rec, z.S);
     if (!(fabsf(top) < INFINITY) || !(st.temp >= 0.f)) return no_distribution(a, r);
@@ -1431,7 +1446,8 @@ size_t token_sample_workspace_bytes(int R, int V, int) { return layout_of(R, V).
 hipError_t launch_token_sample(const TokenSample &a, bool bf16, hipStream_t stream)
 {
     const Layout y = layout_of(a.R, a.V);
-    if (y.S) return bf16 ? launch_slices<uint16_t>(a, y, stream) : launch_slices<float>(a, y, stream);
+    const bool top_k = a.top_k && !a.top_p && a.V <= kSliceFromTopK;
+    if (y.S && !top_k) return bf16 ? launch_slices<uint16_t>(a, y, stream) : launch_slices<float>(a, y, stream);
     const dim3 gd((unsigned)a.R), bd(Block<16>::kBlock);
     if (bf16) hipLaunchKernelGGL(token_sample_kernel<uint16_t>, gd, bd, 0, stream, a);
     else hipLaunchKernelGGL(token_sample_kernel<float>, gd, bd, 0, stream, a);
