@@ -934,7 +934,10 @@ constexpr int kSliceFromTopK = 131072;
 constexpr int kLoads = 4;                              // loads of four logits a thread
 constexpr int kSlice = 4 * kLoads * B::kBlock;         // logits of a slice: 4096
 constexpr int kSlices = 1024;                          // of a row at most
-constexpr int kCandidates = 1024;                      // of a slice, for top-k
+// Of a slice, for top-k: kSliceTopK and the equal or nearly equal logits that come with
+// them; more give the row up.  (Room for 1024 took 4 times the workspace, 268 MB for 32 rows of
+// 2^22 logits, and the same time.)
+constexpr int kCandidates = 256;
 
 struct SliceRecord {
     float top;      // largest logit; +inf: there is a NaN or +inf
