@@ -537,8 +537,9 @@ void fs_postproc_destroy(fs_postproc *pp);
  * pointers of K, V, k, v and the strides multiples of 16 bytes, K and V of at
  * most 64 GiB each, cols * page at most 2^30.  Byte copies: exact.
  * Errors: FS_ERR_INVALID_ARG for negative sizes or strides, page < 1, ld_table
- * < cols, P < 1, N != R without offsets, null or misaligned pointers, or the
- * cache overlapping an input (K and V may be interleaved in one allocation);
+ * < cols, P < 1, N != R without offsets, null or misaligned pointers, the
+ * cache overlapping an input (K and V may be interleaved in one allocation), or
+ * slots of the cache lying on one another (K == V, or a stride of 0);
  * FS_ERR_UNSUPPORTED for what lies outside the set above; FS_ERR_HIP for a
  * failed launch.  N, R or Hkv == 0 returns FS_OK with no launch.
  */
@@ -591,10 +592,11 @@ size_t fs_paged_attn_workspace_bytes(int R, int Hq, int Hkv, int page, int cols,
  * Supported: fs_paged_append's set; Hq a multiple of Hkv, R * Hq <= 2^24.
  * Arithmetic: weights, products and sums in fp32, one rounding at the end.  The
  * bits depend on the data and the sizes, never on run or launch.
- * Errors: those of fs_paged_append; FS_ERR_INVALID_ARG also for Hq not a
- * multiple of Hkv, one of k and v without the other, a scale that is not
- * finite, a workspace that is too small or misaligned, or out or the workspace
- * overlapping another argument.  R or Hq == 0 returns FS_OK with no launch.
+ * Errors: those of fs_paged_append (slots on one another: only with k and v);
+ * FS_ERR_INVALID_ARG also for Hq not a multiple of Hkv, one of k and v without
+ * the other, a scale that is not finite, a workspace that is too small or
+ * misaligned, or out or the workspace overlapping another argument.  R or Hq
+ * == 0 returns FS_OK with no launch.
  */
 int fs_paged_attn(const void *q, int64_t q_row_stride, int64_t q_head_stride, void *K, void *V, int64_t page_stride,
                   int64_t head_stride, int64_t slot_stride, int P, int page, const int32_t *table, int ld_table, int cols,

@@ -724,6 +724,16 @@ int check_paged(const void *K, const void *V, int64_t page_stride, int64_t head_
     return FS_OK;
 }
 
+// A written cache's slots are apart: not the same K and V, none of the dimensions expanded.
+int check_paged_written(const void *K, const void *V, int64_t page_stride, int64_t head_stride, int64_t slot_stride,
+                        int P, int page, int Hkv)
+{
+    if (K == V || (P > 1 && page_stride == 0) || (Hkv > 1 && head_stride == 0) || (page > 1 && slot_stride == 0))
+        return fail(FS_ERR_INVALID_ARG, "slots of a written cache lie on one another (K=%p V=%p strides %lld %lld %lld)", K, V,
+                    (long long)page_stride, (long long)head_stride, (long long)slot_stride);
+    return FS_OK;
+}
+
 int check_paged_sizes(int R, int Hkv, int P, int page, int ld_table, int cols, int D, int dtype) {
     if (R < 0 || Hkv < 0 || P < 0 || ld_table < 0 || cols < 0 || D < 0)
         return fail(FS_ERR_INVALID_ARG, "negative size (R=%d Hkv=%d P=%d ld_table=%d cols=%d D=%d)", R, Hkv, P, ld_table,
@@ -788,6 +798,7 @@ int fs_paged_append(void *K, void *V, int64_t page_stride, int64_t head_stride, 
         return fail(FS_ERR_UNSUPPORTED, "Hkv=%d heads of D=%d are more than 2^28 bytes a token", Hkv, D);
     if ((long long)N * Hkv * (D * (int)esize / 16) > (long long)INT_MAX * 128)
         return fail(FS_ERR_UNSUPPORTED, "too many tokens for one launch (N=%d Hkv=%d D=%d)", N, Hkv, D);
+    if ((st = check_paged_written(K, V, page_stride, head_stride, slot_stride, P, page, Hkv)) != FS_OK) return st;
     for (const void *c : {(const void *)K, (const void *)V})
         if (overlaps(c, kv_bytes, k, new_bytes) || overlaps(c, kv_bytes, v, new_bytes) ||
             overlaps(c, kv_bytes, table, table_bytes) || overlaps(c, kv_bytes, start, (size_t)R * 4) ||
@@ -846,12 +857,14 @@ int fs_paged_attn(const void *q, int64_t q_row_stride, int64_t q_head_stride, vo
         overlaps(out, out_bytes, kv_len, (size_t)R * 4) || overlaps(out, out_bytes, k, new_bytes) ||
         overlaps(out, out_bytes, v, new_bytes))
         return fail(FS_ERR_INVALID_ARG, "out overlaps an input");
-    if (k)
+    if (k) {
+        if ((st = check_paged_written(K, V, page_stride, head_stride, slot_stride, P, page, Hkv)) != FS_OK) return st;
         for (const void *c : {(const void *)K, (const void *)V})
             if (overlaps(c, kv_bytes, k, new_bytes) || overlaps(c, kv_bytes, v, new_bytes) ||
                 overlaps(c, kv_bytes, q, q_bytes) || overlaps(c, kv_bytes, table, table_bytes) ||
                 overlaps(c, kv_bytes, kv_len, (size_t)R * 4))
                 return fail(FS_ERR_INVALID_ARG, "the cache overlaps an input");
+    }
     const size_t need = fs::paged_attn_workspace_bytes(R, Hq, Hkv, page, cols, D);
     if (workspace_bytes < need || !workspace)
         return fail(FS_ERR_INVALID_ARG, "workspace of %zu bytes at %p; %zu bytes needed", workspace_bytes, workspace, need);
