@@ -581,7 +581,8 @@ size_t fs_paged_attn_workspace_bytes(int R, int Hq, int Hkv, int page, int cols,
  *   kv_len       [R] int32
  *   k, v         [R, Hkv, D] dtype, strides new_row_stride and
  *                new_head_stride, or NULL
- *   scale        factor of the scores (1 / sqrt(D) as a rule), finite
+ *   scale        factor of the scores (1 / sqrt(D) as a rule); scale * log2(e)
+ *                finite, for the scores are taken in base 2 (in fp32)
  *   out          [R, Hq, D] dtype, contiguous
  *   workspace, workspace_bytes  at least fs_paged_attn_workspace_bytes bytes,
  *                zero-filled before its first use and written by nothing but
@@ -594,7 +595,7 @@ size_t fs_paged_attn_workspace_bytes(int R, int Hq, int Hkv, int page, int cols,
  * bits depend on the data and the sizes, never on run or launch.
  * Errors: those of fs_paged_append (slots on one another: only with k and v);
  * FS_ERR_INVALID_ARG also for Hq not a multiple of Hkv, one of k and v without
- * the other, a scale that is not finite, a workspace that is too small or
+ * the other, scale * log2(e) not finite, a workspace that is too small or
  * misaligned, or out or the workspace overlapping another argument.  R or Hq
  * == 0 returns FS_OK with no launch.
  */

@@ -828,8 +828,9 @@ int fs_paged_attn(const void *q, int64_t q_row_stride, int64_t q_head_stride, vo
     int st = check_paged_sizes(R, Hkv, P, page, ld_table, cols, D, dtype);
     if (st != FS_OK) return st;
     if ((st = check_paged_attn_sizes(R, Hq, Hkv, page, cols, D, dtype)) != FS_OK) return st;
-    if (!(scale > -std::numeric_limits<float>::infinity() && scale < std::numeric_limits<float>::infinity()))
-        return fail(FS_ERR_INVALID_ARG, "scale is not finite");
+    const float base2 = scale * 1.44269504f;   // what the scores are multiplied with
+    if (!(base2 > -std::numeric_limits<float>::infinity() && base2 < std::numeric_limits<float>::infinity()))
+        return fail(FS_ERR_INVALID_ARG, "scale * log2(e) is not finite");
     if (R == 0 || Hq == 0) return FS_OK;
     const size_t esize = dtype == FS_BF16 ? 2 : 4;
     size_t kv_bytes = 0, table_bytes = 0;

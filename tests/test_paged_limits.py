@@ -15,6 +15,12 @@ def test_sampling_workspace_of_many_logits():
         assert N.lib().fs_token_sample_workspace_bytes(R, V, N.FS_F32) <= R * (40_000 + 3 * V // 4)
 
 
+@pytest.mark.parametrize("scale", [3e38, -2.4e38])
+def test_a_scale_that_overflows_in_base_2_is_refused(scale):
+    """Scores are taken in base 2: with a factor of infinity a product of 0 would be NaN."""
+    assert attn(scale=scale) == INVALID and "scale" in N.last_error()
+
+
 @pytest.mark.parametrize("change,needle", [
     (dict(V=BIG), "one another"), (dict(ps=0), "one another"), (dict(hs=0), "one another"), (dict(ss=0), "one another"),
 ])
