@@ -41,6 +41,7 @@
 
 
 #include "div.h"
+#include "grid.h"
 #include "launch.h"
 #include "trace.h"
 
@@ -885,6 +886,7 @@ hipError_t launch_beam_select(const float *logits, const float *beam_scores, con
     const int NS = beam_select_slices(rows, V, k, c);
     const int SL = (V + NS - 1) / NS;
     const long long nblk = (long long)rows * NS + B;
+    if (!one_dimension(nblk, kThreads)) return hipErrorInvalidConfiguration;
     unsigned long long *ctr = workspace + (size_t)rows * NS * rec_words(c);
     const Div ns = make_div(NS), dk = make_div(k), dc = make_div(c), dv = make_div(V);
     auto launch = [&](auto kernel) {

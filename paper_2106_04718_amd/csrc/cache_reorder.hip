@@ -17,6 +17,7 @@
 // written.
 #include <stdint.h>
 
+#include "grid.h"
 #include "launch.h"
 
 typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
@@ -184,6 +185,7 @@ hipError_t launch_ancestry_step(int32_t *anc, int ld, const int32_t *parent, int
                                 hipStream_t stream)
 {
     const int nblk = (t + 1 + kThreads - 1) / kThreads;
+    if (!one_dimension((long long)B * nblk, kThreads)) return hipErrorInvalidConfiguration;
     const dim3 gd((unsigned)((long long)B * nblk)), bd(kThreads);
     if (k <= 4)
         hipLaunchKernelGGL(ancestry_step_kernel<4>, gd, bd, 0, stream, anc, ld, parent, k, t, nblk);

@@ -48,6 +48,7 @@
 #include <type_traits>
 
 #include "div.h"
+#include "grid.h"
 #include "launch.h"
 #include "ngram_row.h"
 #include "trace.h"
@@ -1617,6 +1618,7 @@ hipError_t launch_split(const AttnArgs &a, int NC)
     ng.blocks = ng.rows > 0 ? (ng.rows + kWaves - 1) / kWaves : 0;
     ng.blocks = (ng.blocks + kXcds - 1) / kXcds * kXcds;
     const long long nblk = ng.blocks + (SPLIT ? n_bh8 : 0) + n_bh8 * NC + mergers;
+    if (!one_dimension(nblk, kBlock)) return hipErrorInvalidConfiguration;
     const Div dv = make_div(a.H);
     hipLaunchKernelGGL((cross_attn_kernel<D, BF16, KB, SPLIT, ANC, BM>), dim3((unsigned)nblk), dim3(kBlock), 0,
                        a.stream, static_cast<const uint4 *>(a.q), static_cast<const uint4 *>(a.K),
@@ -1633,6 +1635,7 @@ hipError_t launch_whole(const AttnArgs &a)
     const double scale_log2 = 1.4426950408889634074 / sqrt((double)D);
     NgramJob ng = a.ng;
     ng.blocks = ng.rows > 0 ? (ng.rows + kWaves * P - 1) / (kWaves * P) : 0;
+    if (!one_dimension((long long)ng.blocks + n_bh, kBlock * P)) return hipErrorInvalidConfiguration;
     const Div dv = make_div(a.H);
     hipLaunchKernelGGL((attn_whole_kernel<D, BF16, KB, SPLIT, P, ANC, BM>), dim3((unsigned)(ng.blocks + n_bh)),
                        dim3(kBlock * P), 0,

@@ -15,6 +15,10 @@ inline dim3 wide_grid(long long workgroups) {
     if (workgroups <= kGridRow) return dim3((unsigned)workgroups);
     return dim3(kGridRow, (unsigned)((workgroups + kGridRow - 1) / kGridRow));
 }
+
+// Kernels that number their workgroups along one dimension: whether that holds them.
+inline bool one_dimension(long long workgroups, unsigned lanes) { return workgroups * lanes <= 0xffffffffll; }
+
 __device__ __forceinline__ unsigned wide_index() { return blockIdx.y * kGridRow + blockIdx.x; }
 
 }  // namespace fs

@@ -19,6 +19,7 @@
 // are needed.
 #include <math.h>
 
+#include "grid.h"
 #include "launch.h"
 
 namespace fs {
@@ -105,6 +106,7 @@ void launch_fixed(const int32_t *tokens, int ld, int rows, int t, float *logits,
 hipError_t launch_ngram_block(const int32_t *tokens, int ld_tokens, int rows, int t, int n,
                               float *logits, int V, hipStream_t stream)
 {
+    if (!one_dimension(rows, kWave)) return hipErrorInvalidConfiguration;
     switch (n - 1) {
     case 0: launch_fixed<0>(tokens, ld_tokens, rows, t, logits, V, stream); break;
     case 1: launch_fixed<1>(tokens, ld_tokens, rows, t, logits, V, stream); break;
