@@ -522,7 +522,7 @@ void fs_postproc_destroy(fs_postproc *pp);
  * A token is skipped where pos < 0, pos / page >= cols or pg lies outside
  * [0, P).  Tokens of no row (before offsets[0], behind offsets[R]) are skipped,
  * so k and v may be padded.  Nothing else of the cache is written.  Two tokens
- * that name one slot leave either one's row there.
+ * that name one slot leave parts of either one's row there.
  *
  * Arguments (device pointers except the sizes; strides in elements):
  *   K, V         dtype, updated in place; both with strides page_stride,
@@ -639,8 +639,10 @@ size_t fs_token_sample_workspace_bytes(int R, int V, int dtype);
  *   stream       hipStream_t (NULL = default stream)
  * Supported: dtype FS_F32 or FS_BF16, 1 <= V <= 2^24, R <= 2^20.
  * Arithmetic: weights and sums in 64 bits; top-p's mass as whole numbers of
- * 2^-44 of the largest weight (V <= 2^18; 2^(18 - log2 V) times as coarse
- * above), so a draw depends on the data alone, never on run or launch.
+ * 2^-44 of the largest weight (V <= 2^18; 2^(log2 V - 18) times as coarse
+ * above).  A draw depends on the data, and within the sums' rounding of a border
+ * on R, V and which settings are NULL (they order the sums), never on run or
+ * launch.
  * Errors: FS_ERR_INVALID_ARG for negative sizes, V < 1, ld_logits < V, null or
  * misaligned pointers, a workspace that is too small, or an output or the
  * workspace overlapping another argument; FS_ERR_UNSUPPORTED for dtype, V or R

@@ -31,11 +31,11 @@
 //   parts of the part that has the token.
 //
 // Two ways through a row.
-//   sample_row     one workgroup has it and reads it two or three times, after the
-//                  first time from the caches (held in registers, it needs unrolled
-//                  passes, which run once a row: waiting for their instructions cost
-//                  more than reading again).  For many rows, and for the rows that
-//                  the other way gives up.
+//   sample_row     one workgroup has it and reads it two to four times (with the
+//                  search by digits seven to fifteen), after the first time from the
+//                  caches (held in registers, it needs unrolled passes, which run once a
+//                  row: waiting for their instructions cost more than reading again).
+//                  For many rows, and for the rows that the other way gives up.
 //   four kernels   with a workgroup per slice of 4096 logits, for up to
 //                  kSliceRows rows of more than kSliceFrom logits (and, with
 //                  top-k, of small k):
@@ -51,9 +51,9 @@
 //                  One row of 131072 then is on 32 CUs, and the bins' atomic
 //                  additions, which are what a CU's LDS is slowest at, with it.
 //
-// Measured: 128 rows of 50264 with top-k and top-p 17.4 us, 512 bf16 rows of 50257
-// without a filter 44, 256 rows of 151936 with settings of their own 153, one row of
-// 131072 with top-p 33.
+// Measured, calls back to back: 128 rows of 50264 with top-k and top-p 17.7 us, 512 bf16
+// rows of 50257 without a filter 44 (one launch by itself 48), 256 rows of 151936 with
+// settings of their own 154, one row of 131072 with top-p 33.
 #include <math.h>
 #include <stdint.h>
 
