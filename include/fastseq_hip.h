@@ -39,6 +39,11 @@
  *                       own key and value and write them.
  *   fs_token_sample     one token per row by temperature, top-k, top-p and
  *                       min-p, from given random numbers.
+ *   fs_paged_resize     rows of the cache grow and shrink: their pages, and the
+ *                       positions and slots of new tokens.
+ *   fs_rotary           queries and keys turned by their positions.
+ *   fs_paged_chunk_attn causal attention of several new tokens per row (pieces
+ *                       of prompts, drafted tokens) over that cache.
  *
  * Conventions shared by every entry point
  *   - Pointers named "device" are HIP device memory; the caller owns every
@@ -604,6 +609,159 @@ int fs_paged_attn(const void *q, int64_t q_row_stride, int64_t q_head_stride, vo
                   const int32_t *kv_len, const void *k, const void *v, int64_t new_row_stride, int64_t new_head_stride,
                   float scale, void *out, int R, int Hq, int Hkv, int D, int dtype, void *workspace,
                   size_t workspace_bytes, void *stream);
+
+/* Workspace, in bytes, that fs_paged_resize needs for these sizes.  Any contents
+ * will do, and any later call that fits may reuse it.  0 for R == 0 and N == 0;
+ * (size_t)-1 for invalid or unsupported sizes. */
+size_t fs_paged_resize_workspace_bytes(int R, int N);
+
+/*
+ * Rows of a paged cache grow and shrink: pages are taken from a stack of free
+ * ones and given back, and every new token gets its position and its slot.
+ *
+ * Row r holds L = clamp(kv_len[r], 0, cols * page) positions in its first
+ * ceil(L / page) pages, which are its alone, and is to hold W = max(want[r], 0).
+ *   - A row that shrinks gives back its pages from ceil(W / page) on: those in
+ *     [0, P) go on the stack, the last row's last page first, so that growing
+ *     again at once finds the same pages in the same places.  The entries of the
+ *     table become -1.
+ *   - Then rows that grow take pages from the top of the stack, in their order.  A
+ *     row is granted if W <= cols * page and it needs no page, or the pages that
+ *     it and the rows before it need (those with W <= cols * page) are there.
+ * kv_len[r] becomes W where the row shrank, stayed or was granted, and is left as it
+ * was, like its pages, where it was refused.
+ *
+ * The tokens to be added, A = max(0, W - L) of each row (granted or not), are
+ * numbered row by row:
+ *     start[r] = L        offsets[r] = sum of A of the rows before r (r = 0 .. R;
+ *                         no more than 2^31 - 1)
+ *     positions[n] = start[r] + n - offsets[r]       for the tokens n of row r
+ *     slots[n] = table[r, positions[n] / page] * page + positions[n] % page
+ * slots[n] is -1 where the row was refused or its page is none of [0, P).
+ * Entries of no token get position 0 and slot -1.  start and offsets are what
+ * fs_paged_append takes, positions what fs_rotary takes.
+ *
+ * Arguments (device pointers except the sizes):
+ *   table        [R, cols] int32, leading dimension ld_table >= cols
+ *   kv_len       [R] int32, updated in place; want [R] int32
+ *   free_pages   [P] int32, a stack whose top is entry free_count[0] - 1; P is the
+ *                number of the cache's pages.  Entries from free_count on are not
+ *                kept.  A count outside [0, P] is taken as the nearer of them.
+ *   free_count   [1] int32, updated in place
+ *   start [R], offsets [R + 1], positions [N] int32, slots [N] int64; each may be
+ *                NULL
+ *   N            entries of positions and slots
+ *   workspace, workspace_bytes  at least fs_paged_resize_workspace_bytes bytes.
+ *                Calls that share a workspace must not run concurrently.
+ *   stream       hipStream_t (NULL = default stream)
+ * Supported: R <= 2^20, R * cols < 2^31, cols * page <= 2^30.  Whole numbers: the
+ * same on every run.
+ * Errors: FS_ERR_INVALID_ARG for negative sizes, page < 1, ld_table < cols, null
+ * or misaligned pointers, a workspace that is too small or arguments that overlap;
+ * FS_ERR_UNSUPPORTED for what lies outside the set above; FS_ERR_HIP for a failed
+ * launch.  R == 0 and N == 0 returns FS_OK with no launch.
+ */
+int fs_paged_resize(int32_t *table, int ld_table, int cols, int32_t *kv_len, const int32_t *want, int R, int page,
+                    int32_t *free_pages, int32_t *free_count, int P, int32_t *start, int32_t *offsets, int32_t *positions,
+                    int64_t *slots, int N, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Frequencies for fs_rotary, on the host: with f = base^(-2i / rot),
+ *     freq[i] = f (1 - g) / factor + f g          i < rot / 2
+ * radians a position.  context == 0: g = 0, every position is divided by factor.
+ * context > 0: by the turns that pair i makes over that many positions,
+ *     g = clamp((context * f / (2 pi) - slow) / (fast - slow), 0, 1)
+ * so that pairs of more than `fast` turns (32 as a rule) keep their frequency and
+ * those of fewer than `slow` (1) are divided (YaRN, arXiv 2309.00071, Section 3.2;
+ * its factor of queries and keys, 0.1 ln(factor) + 1, is fs_rotary's magnitude).
+ * Errors: FS_ERR_INVALID_ARG for rot odd or negative, base or factor not positive
+ * and finite, context < 0, fast <= slow or slow < 0 with context > 0, freq null.
+ */
+int fs_rotary_frequencies(double *freq, int rot, double base, double factor, int context, double fast, double slow);
+
+/*
+ * Rotary positions: pair i of every head of token n is turned by the angle
+ * t = positions[n] * freq[i],
+ *     a' = magnitude (a cos t - b sin t)      b' = magnitude (b cos t + a sin t)
+ * a and b being elements i and i + rot / 2 of the head, or with interleaved != 0
+ * elements 2i and 2i + 1 (i < rot / 2).  Elements from rot on stay as they are.
+ * Negative positions turn back.
+ *
+ * Arguments (device pointers except the sizes; strides in elements):
+ *   q            [N, Hq, D] dtype, strides q_token_stride and q_head_stride
+ *   k            [N, Hkv, D] dtype, strides k_token_stride and k_head_stride; may be
+ *                NULL with Hkv == 0
+ *   positions    [N] int32
+ *   freq         [rot / 2] fp64, radians a position
+ *   q_out, k_out as q and k, with strides of their own; q_out may be q and k_out
+ *                k, with the same strides (in place: elements from rot on are then
+ *                not touched)
+ *   stream       hipStream_t (NULL = default stream)
+ * Supported: dtype FS_F32 or FS_BF16, D in {16, 32, 64, 128}, rot even and <= D,
+ * Hq + Hkv <= 2^17, pointers and strides of q, k and the outputs multiples of 16
+ * bytes.
+ * Arithmetic: angles in fp64 and reduced there, cosines, sines, products and sums
+ * in fp32, one rounding at the end.
+ * Errors: FS_ERR_INVALID_ARG for negative sizes or strides, rot odd, negative or above
+ * D, interleaved neither 0 nor 1, null or misaligned pointers, rows of an output that lie
+ * on one another, or an output overlapping an input (but for itself in place) or the
+ * other output; arrays cut from one projection may lie within one another's extent.
+ * FS_ERR_UNSUPPORTED for what lies outside the set above; FS_ERR_HIP for a failed
+ * launch.  N == 0 or Hq == Hkv == 0 returns FS_OK with no launch.
+ */
+int fs_rotary(const void *q, int64_t q_token_stride, int64_t q_head_stride, const void *k, int64_t k_token_stride,
+              int64_t k_head_stride, const int32_t *positions, const double *freq, int rot, int interleaved, float magnitude,
+              void *q_out, int64_t q_out_token_stride, int64_t q_out_head_stride, void *k_out, int64_t k_out_token_stride,
+              int64_t k_out_head_stride, int N, int Hq, int Hkv, int D, int dtype, void *stream);
+
+/*
+ * Workspace, in bytes, that fs_paged_chunk_attn needs for these sizes.  Zero-fill it
+ * before its first use; a call leaves its counters at zero again, so any later call
+ * that fits may reuse it.  0 for empty problems; (size_t)-1 for invalid or
+ * unsupported sizes.
+ */
+size_t fs_paged_chunk_attn_workspace_bytes(int N, int R, int Hq, int Hkv, int page, int cols, int D, int dtype);
+
+/*
+ * Causal attention of several new tokens per row over a paged cache that holds
+ * their keys and values already (fs_paged_append).
+ *
+ * Row r's tokens are n = offsets[r] .. offsets[r+1] - 1 of q: the last of its
+ * kv_len[r] positions.  Token n is position p = kv_len[r] - offsets[r+1] + n and
+ * attends the positions up to its own: with query head h reading key-value head
+ * g = h / (Hq / Hkv) and pg(j) = table[r, j / page],
+ *     s_j         = scale * (q[n,h,:] . K[pg(j), g, j % page, :])     j <= p
+ *     out[n,h,:]  = sum_j softmax(s)_j * V[pg(j), g, j % page, :]
+ * over the j < cols * page whose pg(j) lies in [0, P); out[n,h,:] = 0 where there is
+ * none (p < 0 among them).  Nothing behind p reaches a token, infinities and NaN
+ * included.  An infinite value among the attended ones gives an infinity or NaN.
+ * With one token per row it is fs_paged_attn without k and v.  Tokens of no row
+ * (before offsets[0], behind offsets[R]) are neither read nor written, so q and out
+ * may be padded.
+ *
+ * Arguments (device pointers except the sizes; strides in elements):
+ *   q            [N, Hq, D] dtype, strides q_token_stride and q_head_stride
+ *   K, V, table  as for fs_paged_append; only read
+ *   kv_len       [R] int32, the row's new tokens included
+ *   offsets      [R + 1] int32, not decreasing
+ *   scale        as for fs_paged_attn
+ *   out          [N, Hq, D] dtype, contiguous
+ *   workspace, workspace_bytes  at least fs_paged_chunk_attn_workspace_bytes bytes,
+ *                zero-filled before its first use and written by nothing but this
+ *                call.  Calls that share a workspace must not run concurrently;
+ *                calls of any sizes that fit may follow each other, eagerly or
+ *                replayed from graphs.
+ *   stream       hipStream_t (NULL = default stream)
+ * Supported: fs_paged_append's set; Hq a multiple of Hkv, N * Hq <= 2^28, R <= 2^24.
+ * Arithmetic: products and sums in fp32, one rounding at the end.  The bits depend on
+ * the data and the sizes, never on run or launch.
+ * Errors: those of fs_paged_attn for the arguments that both have.  N, R or Hq == 0
+ * returns FS_OK with no launch.
+ */
+int fs_paged_chunk_attn(const void *q, int64_t q_token_stride, int64_t q_head_stride, const void *K, const void *V,
+                        int64_t page_stride, int64_t head_stride, int64_t slot_stride, int P, int page, const int32_t *table,
+                        int ld_table, int cols, const int32_t *kv_len, const int32_t *offsets, float scale, void *out, int N, int R,
+                        int Hq, int Hkv, int D, int dtype, void *workspace, size_t workspace_bytes, void *stream);
 
 /* Workspace, in bytes, that fs_token_sample needs for these sizes.  Zero-fill
  * it before its first use; any later call that fits may reuse it.  0 for

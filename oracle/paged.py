@@ -7,6 +7,10 @@ library.  Caches are [P, Hkv, page, D] arrays, bf16 values as their uint16 bits.
   follow those their rows hold.
 * :func:`paged_attn` -- softmax attention of one query per head over the
   positions that a row's table names.
+* :func:`paged_resize` -- rows that grow and shrink: their pages, and the positions
+  and slots of new tokens.
+* :func:`rotary`, :func:`rotary_frequencies` -- heads turned by their positions.
+* :func:`paged_chunk_attn` -- causal attention of several new tokens per row.
 * :func:`token_sample` -- the draw of one token per row by temperature, top-k,
   top-p and min-p from a given uniform number.
 """
@@ -69,6 +73,97 @@ def paged_attn(q, K, V, table, kv_len, k=None, v=None, scale=None):
                 p = np.exp(s - s.max())
                 out[r, h] = (p / p.sum()) @ vv
     return (out, K, V) if k is not None else out
+
+
+def paged_resize(table, kv_len, want, free_pages, free_count, page, N=0):
+    """The state after the call (copies) and what it says of the tokens, as a dict."""
+    table, kv_len, free = table.copy(), kv_len.copy(), free_pages.copy()
+    R, cols = table.shape
+    P, cap = len(free), cols * page
+    count = min(max(int(free_count), 0), P)
+    held = [min(max(int(x), 0), cap) for x in kv_len]
+    wants = [max(int(x), 0) for x in want]
+    pages = lambda n: -(-n // page)
+    for r in reversed(range(R)):
+        for j in reversed(range(pages(wants[r]), pages(held[r]))):
+            if 0 <= table[r, j] < P:
+                if count < P:
+                    free[count] = table[r, j]
+                count += 1
+            table[r, j] = -1
+    count = min(count, P)
+    needed, top, granted = 0, count, []
+    for r in range(R):
+        more = pages(wants[r]) - pages(held[r])
+        ok = wants[r] <= cap
+        if ok and more > 0:
+            needed += more
+            ok = needed <= top
+        granted.append(ok)
+        if ok:
+            for j in range(pages(held[r]), pages(wants[r])):
+                count -= 1
+                table[r, j] = free[count]
+            kv_len[r] = wants[r]
+    off = [0]
+    for r in range(R):
+        off.append(off[-1] + max(0, wants[r] - held[r]))
+    positions, slots = np.zeros(N, np.int32), np.full(N, -1, np.int64)
+    for r in range(R):
+        for n in range(off[r], min(off[r + 1], N)):
+            pos = positions[n] = held[r] + n - off[r]
+            if granted[r] and 0 <= table[r, pos // page] < P:
+                slots[n] = int(table[r, pos // page]) * page + pos % page
+    return dict(table=table, kv_len=kv_len, free_pages=free, free_count=count, start=np.array(held, np.int32),
+                offsets=np.minimum(np.array(off, np.int64), 2**31 - 1).astype(np.int32), positions=positions, slots=slots)
+
+
+def rotary_frequencies(rot, base=10000.0, factor=1.0, context=0, fast=32.0, slow=1.0):
+    out = []
+    for i in range(rot // 2):
+        f = base ** (-2 * i / rot)
+        g = min(1.0, max(0.0, (context * f / (2 * math.pi) - slow) / (fast - slow))) if context else 0.0
+        out.append(f / factor * (1 - g) + f * g)
+    return np.array(out)
+
+
+def rotary(x, positions, freq, interleaved=False, magnitude=1.0):
+    """x [N, H, D] turned, fp64."""
+    x = _f64(x)
+    out, half = x.copy(), len(freq)
+    for n, p in enumerate(positions):
+        for i, f in enumerate(freq):
+            a, b = (2 * i, 2 * i + 1) if interleaved else (i, i + half)
+            z = (x[n, :, a] + 1j * x[n, :, b]) * magnitude * complex(math.cos(int(p) * f), math.sin(int(p) * f))
+            out[n, :, a], out[n, :, b] = z.real, z.imag
+    return out
+
+
+def paged_chunk_attn(q, K, V, table, kv_len, offsets, scale=None):
+    """out [N, Hq, D] fp64 (NaN for tokens of no row), and the softmax-weighted mean of the
+    values' magnitudes, of the same shape."""
+    N, Hq, D = q.shape
+    P, Hkv, page = K.shape[:3]
+    scale = D ** -0.5 if scale is None else scale
+    out, mean = np.full((N, Hq, D), np.nan), np.zeros((N, Hq, D))
+    cap = table.shape[1] * page
+    for r in range(table.shape[0]):
+        lo, hi = int(offsets[r]), int(offsets[r + 1])
+        for n in range(lo, hi):
+            p = max(int(kv_len[r]), 0) - hi + n
+            out[n] = 0
+            slots = [s for s in (_slot(table, r, j, page, P) for j in range(min(p + 1, cap))) if s is not None]
+            if not slots:
+                continue
+            pg, sl = np.array(slots).T
+            for g in range(Hkv):
+                kk, vv = _f64(K[pg, g, sl]), _f64(V[pg, g, sl])
+                hs = slice(g * (Hq // Hkv), (g + 1) * (Hq // Hkv))
+                s = scale * (_f64(q[n, hs]) @ kk.T)
+                w = np.exp(s - s.max(1, keepdims=True))
+                w /= w.sum(1, keepdims=True)
+                out[n, hs], mean[n, hs] = w @ vv, w @ np.abs(vv)
+    return out, mean
 
 
 def token_sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None):

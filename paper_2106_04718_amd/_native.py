@@ -59,6 +59,16 @@ SIGNATURES = [
     ("fs_paged_attn", _c_int,
      [_vp] + [_c_i64] * 2 + [_vp] * 2 + [_c_i64] * 3 + [_c_int] * 2 + [_vp] + [_c_int] * 2 + [_vp] * 3 + [_c_i64] * 2 +
      [ctypes.c_float, _vp] + [_c_int] * 5 + [_vp, _c_size, _vp]),
+    ("fs_paged_resize_workspace_bytes", _c_size, [_c_int] * 2),
+    ("fs_paged_resize", _c_int,
+     [_vp] + [_c_int] * 2 + [_vp] * 2 + [_c_int] * 2 + [_vp] * 2 + [_c_int] + [_vp] * 4 + [_c_int, _vp, _c_size, _vp]),
+    ("fs_rotary_frequencies", _c_int, [_vp, _c_int] + [ctypes.c_double] * 2 + [_c_int] + [ctypes.c_double] * 2),
+    ("fs_rotary", _c_int,
+     ([_vp] + [_c_i64] * 2) * 2 + [_vp] * 2 + [_c_int] * 2 + [ctypes.c_float] + ([_vp] + [_c_i64] * 2) * 2 + [_c_int] * 5 + [_vp]),
+    ("fs_paged_chunk_attn_workspace_bytes", _c_size, [_c_int] * 8),
+    ("fs_paged_chunk_attn", _c_int,
+     [_vp] + [_c_i64] * 2 + [_vp] * 2 + [_c_i64] * 3 + [_c_int] * 2 + [_vp] + [_c_int] * 2 + [_vp] * 2 + [ctypes.c_float, _vp] +
+     [_c_int] * 6 + [_vp, _c_size, _vp]),
     ("fs_token_sample_workspace_bytes", _c_size, [_c_int] * 3),
     ("fs_token_sample", _c_int, [_vp, _c_i64] + [_c_int] * 3 + [_vp] * 8 + [_c_size, _vp]),
     ("fs_postproc_create", _c_int,

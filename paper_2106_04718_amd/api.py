@@ -645,6 +645,200 @@ def paged_attn(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, table: torch.T
     return out
 
 
+def paged_resize_workspace_bytes(R: int, N: int) -> int:
+    """Bytes of workspace fs_paged_resize needs for R rows and N tokens."""
+    return _size_or_raise(_native_lib().fs_paged_resize_workspace_bytes(R, N))
+
+
+def paged_resize(table: torch.Tensor, kv_len: torch.Tensor, want: torch.Tensor, free_pages: torch.Tensor,
+                 free_count: torch.Tensor, page: int, start: torch.Tensor | None = None, offsets: torch.Tensor | None = None,
+                 positions: torch.Tensor | None = None, slots: torch.Tensor | None = None,
+                 workspace: torch.Tensor | None = None) -> None:
+    """Rows of a paged cache grow and shrink, in place.
+
+    table [R, cols] int32, the pages of each row, which are its alone; kv_len [R]
+    int32, the positions each row holds, and want [R] int32, those it is to hold;
+    free_pages [P] int32, a stack of the ``free_count`` ([1] int32) pages that are
+    free.  Rows that shrink give their pages back, then rows that grow take theirs, in
+    their order, while there are enough; kv_len of a row that gets none stays as it was.
+    Optional outputs: start [R] int32, the positions held before; offsets [R + 1] int32,
+    the running sums of the tokens added; positions [N] int32 and slots [N] int64, of
+    every token its position and its slot of the cache (page id times ``page`` and the
+    place in it; -1 where it has none).  The exact rules are those of fs_paged_resize in
+    fastseq_hip.h.
+    """
+    if workspace is not None:
+        st = (_fast or _load_fast()).paged_resize(table, kv_len, want, free_pages, free_count, page, start, offsets,
+                                                  positions, slots, workspace)
+        if st is not None:
+            if st:
+                _N.check(st)
+            return
+    _strided("table", table, 2, torch.int32)
+    R, dev = table.shape[0], table.device
+    _int32("kv_len", kv_len, R, dev)
+    _int32("want", want, R, dev)
+    _int32("free_pages", free_pages, free_pages.shape[0] if isinstance(free_pages, torch.Tensor) and free_pages.dim() else 0, dev)
+    _int32("free_count", free_count, 1, dev)
+    if start is not None:
+        _int32("start", start, R, dev)
+    if offsets is not None:
+        _int32("offsets", offsets, R + 1, dev)
+    N = None
+    for name, x, dt in (("positions", positions, torch.int32), ("slots", slots, torch.int64)):
+        if x is None:
+            continue
+        _need_cuda(name, x)
+        if x.dtype != dt or x.dim() != 1 or x.device != dev or (N is not None and x.shape[0] != N):
+            raise ValueError(f"{name} must be {dt} [N] on the table's device")
+        N = x.shape[0]
+    N = N or 0
+    if workspace is None:
+        workspace = new_workspace(paged_resize_workspace_bytes(R, N), dev)
+    else:
+        _need_cuda("workspace", workspace)
+        if workspace.device != dev:
+            raise ValueError("all tensors must be on one device")
+    ptr = lambda x: None if x is None else x.data_ptr()
+    with _on(dev):
+        _N.check(_N.ext().fs_paged_resize(
+            table.data_ptr(), table.stride(0) if R > 1 else table.shape[1], table.shape[1], kv_len.data_ptr(), want.data_ptr(),
+            R, int(page), free_pages.data_ptr(), free_count.data_ptr(), free_pages.shape[0], ptr(start), ptr(offsets),
+            ptr(positions), ptr(slots), N, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+            _stream_ptr(dev)))
+
+
+def rotary_frequencies(rot: int, base: float = 10000.0, factor: float = 1.0, context: int = 0, fast: float = 32.0,
+                       slow: float = 1.0, device=None) -> torch.Tensor:
+    """Frequencies for :func:`rotary`, [rot / 2] float64, in radians a position:
+    base ** (-2 i / rot).  With ``factor`` they are scaled for contexts that many times as
+    long: all of them divided by it, or with ``context`` (the length that they were made for)
+    those of pairs that turn fewer than ``slow`` times over it, the ones of more than ``fast``
+    turns kept and those between mixed.
+    """
+    freq = torch.empty(max(0, int(rot) // 2), dtype=torch.float64)
+    _N.check_lib(_N.lib().fs_rotary_frequencies(freq.data_ptr(), int(rot), float(base), float(factor), int(context),
+                                                float(fast), float(slow)))
+    return freq.to(device) if device is not None else freq
+
+
+def _rotary_rows(name: str, x: torch.Tensor, like: torch.Tensor) -> None:
+    _strided(name, x, 3, like.dtype, like.device)
+    if x.shape != like.shape:
+        raise ValueError(f"{name} must be {list(like.shape)}")
+
+
+def rotary(q: torch.Tensor, positions: torch.Tensor, freq: torch.Tensor, k: torch.Tensor | None = None,
+           out: torch.Tensor | None = None, k_out: torch.Tensor | None = None, interleaved: bool = False,
+           magnitude: float = 1.0):
+    """Queries and keys turned by their positions.
+
+    q [N, Hq, D] and k [N, Hkv, D] float32 or bfloat16 (contiguous rows); positions [N]
+    int32; freq [rot / 2] float64 (:func:`rotary_frequencies`).  Pair i of every head is
+    turned by positions[n] * freq[i] and multiplied with ``magnitude``; pairs are elements
+    i and i + rot / 2 of the head, or 2i and 2i + 1 with ``interleaved``; elements from rot
+    on stay as they are.  ``out`` and ``k_out`` pass the outputs; they may be q and k
+    themselves.  Returns out, or (out, k_out) with ``k``.
+    """
+    if out is not None and (k is None or k_out is not None):
+        st = (_fast or _load_fast()).rotary(q, positions, freq, k, interleaved, magnitude, out, k_out)
+        if st is not None:
+            if st:
+                _N.check(st)
+            return out if k is None else (out, k_out)
+    _strided("q", q, 3)
+    if q.dtype not in _DTYPES:
+        raise ValueError("q must be float32 or bfloat16")
+    N, Hq, D = q.shape
+    _need_cuda("positions", positions)
+    if positions.dtype != torch.int32 or positions.shape != (N,) or positions.device != q.device:
+        raise ValueError("positions must be int32 [N] on q's device")
+    _need_cuda("freq", freq)
+    if freq.dtype != torch.float64 or freq.dim() != 1 or freq.device != q.device:
+        raise ValueError("freq must be float64 [rot / 2] on q's device")
+    if out is None:
+        out = torch.empty((N, Hq, D), dtype=q.dtype, device=q.device)
+    else:
+        _rotary_rows("out", out, q)
+    if k is None:
+        if k_out is not None:
+            raise ValueError("k and k_out go together")
+    else:
+        _strided("k", k, 3, q.dtype, q.device)
+        if k.shape[0] != N or k.shape[2] != D:
+            raise ValueError(f"shape mismatch: q{tuple(q.shape)} k{tuple(k.shape)}")
+        if k_out is None:
+            k_out = torch.empty(tuple(k.shape), dtype=k.dtype, device=k.device)
+        else:
+            _rotary_rows("k_out", k_out, k)
+    side = lambda x: (None, 0, 0) if x is None else (x.data_ptr(), x.stride(0), x.stride(1))
+    with _on(q.device):
+        _N.check(_N.ext().fs_rotary(*side(q), *side(k), positions.data_ptr(), freq.data_ptr(), 2 * freq.shape[0],
+                                    int(bool(interleaved)), *side(out), *side(k_out), N, Hq, 0 if k is None else k.shape[1], D,
+                                    _DTYPES[q.dtype], _stream_ptr(q.device), float(magnitude)))
+    return out if k is None else (out, k_out)
+
+
+def paged_chunk_attn_workspace_bytes(N: int, R: int, Hq: int, Hkv: int, page: int, cols: int, D: int,
+                                     dtype: torch.dtype = torch.bfloat16) -> int:
+    """Bytes of workspace fs_paged_chunk_attn needs for these sizes (cols: the table's columns)."""
+    key = ("c", N, R, Hq, Hkv, page, cols, D, dtype)
+    n = _WS_BYTES.get(key)
+    if n is None:
+        n = _size_or_raise(_native_lib().fs_paged_chunk_attn_workspace_bytes(N, R, Hq, Hkv, page, cols, D, _DTYPES[dtype]))
+        _WS_BYTES[key] = n
+    return n
+
+
+def paged_chunk_attn(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, table: torch.Tensor, kv_len: torch.Tensor,
+                     offsets: torch.Tensor, out: torch.Tensor | None = None, workspace: torch.Tensor | None = None,
+                     scale: float | None = None) -> torch.Tensor:
+    """Causal attention of several new tokens per row over a paged cache.
+
+    q [N, Hq, D] (contiguous rows), row r's tokens offsets[r] .. offsets[r+1] - 1 of it
+    (``offsets`` [R + 1] int32); K, V [P, Hkv, page, D] and table [R, cols] as for
+    :func:`paged_append`, Hq a multiple of Hkv; kv_len [R] int32, the positions of each
+    row, its new tokens' included, whose keys and values the cache holds already.  A token
+    attends the positions up to its own.  ``scale`` (default 1 / sqrt(D)) multiplies the
+    scores.  Returns out [N, Hq, D] in the input dtype; zeros where a token attends
+    nothing.  Tokens of no row are left as they are (uninitialised in an ``out`` made here).
+    """
+    if out is not None and workspace is not None:
+        st = (_fast or _load_fast()).paged_chunk_attn(q, K, V, table, kv_len, offsets, out, workspace, scale)
+        if st is not None:
+            if st:
+                _N.check(st)
+            return out
+    ld = _paged_cache(K, V, table)
+    _strided("q", q, 3, K.dtype, K.device)
+    P, Hkv, page, D = K.shape
+    N, Hq = q.shape[0], q.shape[1]
+    R = table.shape[0]
+    if q.shape[2] != D:
+        raise ValueError(f"shape mismatch: q{tuple(q.shape)} K{tuple(K.shape)}")
+    _int32("kv_len", kv_len, R, K.device)
+    _int32("offsets", offsets, R + 1, K.device)
+    if out is None:
+        out = torch.empty((N, Hq, D), dtype=q.dtype, device=q.device)
+    else:
+        _need_cuda("out", out)
+        if out.shape != q.shape or out.dtype != q.dtype or out.device != q.device:
+            raise ValueError("out must match q in shape, dtype and device")
+    if workspace is None:
+        workspace = new_workspace(paged_chunk_attn_workspace_bytes(N, R, Hq, Hkv, page, table.shape[1], D, q.dtype), q.device)
+    else:
+        _need_cuda("workspace", workspace)
+        if workspace.device != q.device:
+            raise ValueError("all tensors must be on one device")
+    with _on(q.device):
+        _N.check(_N.ext().fs_paged_chunk_attn(
+            q.data_ptr(), q.stride(0), q.stride(1), K.data_ptr(), V.data_ptr(), K.stride(0), K.stride(1), K.stride(2), P,
+            page, table.data_ptr(), ld, table.shape[1], kv_len.data_ptr(), offsets.data_ptr(), out.data_ptr(), N, R, Hq, Hkv, D,
+            _DTYPES[q.dtype], workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_ptr(q.device),
+            (D ** -0.5 if D else 1.0) if scale is None else float(scale)))
+    return out
+
+
 def token_sample_workspace_bytes(R: int, V: int, dtype: torch.dtype = torch.float32) -> int:
     """Bytes of workspace fs_token_sample needs for these sizes."""
     key = ("t", R, V, dtype)

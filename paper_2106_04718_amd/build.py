@@ -34,7 +34,7 @@ BUILD = PKG / "_build"
 LIB = PKG / "libfastseq_hip.so"
 EXT = PKG / ("_fastseq_ext" + sysconfig.get_config_var("EXT_SUFFIX"))
 SOURCES = ["capi.cpp", "cross_attn.hip", "ngram_block.hip", "beam_select.hip", "cache_reorder.hip", "paged_append.hip",
-           "paged_attn.hip", "token_sample.hip", "postproc.cpp"]  # pyext.c is built by build_ext
+           "paged_attn.hip", "paged_resize.hip", "paged_chunk.hip", "rotary.hip", "token_sample.hip", "postproc.cpp"]  # pyext.c is built by build_ext
 TORCH_EXT = PKG / ("_fastseq_torch" + sysconfig.get_config_var("EXT_SUFFIX"))
 ARCH = "gfx950"
 

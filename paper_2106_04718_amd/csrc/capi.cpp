@@ -7,6 +7,7 @@
 #include <atomic>
 #include <climits>
 #include <cstdarg>
+#include <cmath>
 #include <cstdint>
 #include <cstdio>
 #include <cstdlib>
@@ -890,6 +891,271 @@ int fs_paged_attn(const void *q, int64_t q_row_stride, int64_t q_head_stride, vo
     a.workspace = static_cast<unsigned char *>(workspace);
     hipError_t err = fs::launch_paged_attn(a, D, dtype == FS_BF16, s);
     if (err != hipSuccess) return hip_fail(err, "fs_paged_attn launch");
+    return FS_OK;
+}
+
+}  // extern "C"
+
+namespace {
+
+// Rows of D contiguous elements, n0 by n1 of them (strides in elements): do no two lie on one another?
+bool rows_apart(long long n0, long long s0, long long n1, long long s1, int D) {
+    if (n0 <= 1) n0 = n1, s0 = s1, n1 = 1;   // one dimension
+    if (n0 <= 1) return true;
+    if (n1 <= 1) return s0 >= D;
+    if (s1 > s0) std::swap(n0, n1), std::swap(s0, s1);
+    return s1 >= D && (__int128)s0 >= (__int128)(n1 - 1) * s1 + D;
+}
+
+// An array of N tokens of H rows of D elements: its strides and its extent, in bytes.
+struct Tokens {
+    const void *p;
+    long long token, head, row, bytes;
+    int H;
+};
+
+// Do the rows of two such arrays (both of N tokens) meet?  Arrays cut from one projection lie
+// within one another's extent: those of one stride between tokens are told apart by their
+// places within it, or within the stride between heads.
+bool tokens_meet(const Tokens &a, const Tokens &b, int N) {
+    if (!overlaps(a.p, (size_t)a.bytes, b.p, (size_t)b.bytes)) return false;
+    const long long d = (long long)(reinterpret_cast<uintptr_t>(b.p) - reinterpret_cast<uintptr_t>(a.p));
+    auto apart = [&](long long stride, long long in_a, long long in_b) {
+        if (stride <= 0) return false;
+        const long long at = (d % stride + stride) % stride;
+        return at >= in_a && at + in_b <= stride;
+    };
+    const auto span = [](const Tokens &x) { return (x.H - 1) * x.head + x.row; };
+    if (N > 1 ? a.token == b.token && apart(a.token, span(a), span(b)) : false) return false;
+    const bool heads = a.H > 1 && b.H > 1 && a.head == b.head && a.head > 0 && (N == 1 || (a.token % a.head == 0 && b.token % b.head == 0));
+    return !(heads && apart(a.head, a.row, b.row));
+}
+
+int check_chunk_sizes(int N, int R, int Hq, int Hkv, int page, int cols, int D, int dtype) {
+    if (N < 0 || Hq < 0) return fail(FS_ERR_INVALID_ARG, "negative size (N=%d Hq=%d)", N, Hq);
+    const int st = check_paged_sizes(R, Hkv, 1, page, cols, cols, D, dtype);
+    if (st != FS_OK) return st;
+    if (Hkv == 0 ? Hq != 0 : Hq % Hkv != 0)
+        return fail(FS_ERR_INVALID_ARG, "Hq=%d is not a multiple of Hkv=%d", Hq, Hkv);
+    if ((long long)N * Hq > (1 << 28)) return fail(FS_ERR_UNSUPPORTED, "N*Hq=%lld exceeds 2^28", (long long)N * Hq);
+    if (R > (1 << 24)) return fail(FS_ERR_UNSUPPORTED, "R=%d rows exceed 2^24", R);
+    if ((long long)cols * page > (1 << 30))
+        return fail(FS_ERR_UNSUPPORTED, "a table of %d pages of %d positions exceeds 2^30 positions", cols, page);
+    return FS_OK;
+}
+
+int check_resize_sizes(int R, int N) {
+    if (R < 0 || N < 0) return fail(FS_ERR_INVALID_ARG, "negative size (R=%d N=%d)", R, N);
+    if (R > (1 << 20)) return fail(FS_ERR_UNSUPPORTED, "R=%d rows exceed 2^20", R);
+    return FS_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t fs_paged_resize_workspace_bytes(int R, int N) {
+    g_last_error.clear();
+    if (check_resize_sizes(R, N) != FS_OK) return (size_t)-1;
+    return R == 0 && N == 0 ? 0 : fs::paged_resize_workspace_bytes(R);
+}
+
+int fs_paged_resize(int32_t *table, int ld_table, int cols, int32_t *kv_len, const int32_t *want, int R, int page,
+                    int32_t *free_pages, int32_t *free_count, int P, int32_t *start, int32_t *offsets, int32_t *positions,
+                    int64_t *slots, int N, void *workspace, size_t workspace_bytes, void *stream)
+{
+    g_last_error.clear();
+    int st = check_resize_sizes(R, N);
+    if (st != FS_OK) return st;
+    if (ld_table < 0 || cols < 0 || P < 0)
+        return fail(FS_ERR_INVALID_ARG, "negative size (ld_table=%d cols=%d P=%d)", ld_table, cols, P);
+    if (page < 1) return fail(FS_ERR_INVALID_ARG, "page=%d < 1", page);
+    if (ld_table < cols) return fail(FS_ERR_INVALID_ARG, "ld_table=%d < cols=%d", ld_table, cols);
+    if ((long long)cols * page > (1 << 30))
+        return fail(FS_ERR_UNSUPPORTED, "a table of %d pages of %d positions exceeds 2^30 positions", cols, page);
+    if ((long long)R * cols > INT_MAX) return fail(FS_ERR_UNSUPPORTED, "a table of R=%d rows of %d pages", R, cols);
+    if (R == 0 && N == 0) return FS_OK;
+    if ((cols > 0 && R > 0 && !table) || (R > 0 && (!kv_len || !want)) || !free_count || (P > 0 && !free_pages))
+        return fail(FS_ERR_INVALID_ARG, "null pointer (table=%p kv_len=%p want=%p free_pages=%p free_count=%p)", (void *)table,
+                    (void *)kv_len, (const void *)want, (void *)free_pages, (void *)free_count);
+    const size_t need = fs::paged_resize_workspace_bytes(R);
+    if (workspace_bytes < need || !workspace)
+        return fail(FS_ERR_INVALID_ARG, "workspace of %zu bytes at %p; %zu bytes needed", workspace_bytes, workspace, need);
+    const size_t rows = (size_t)R * 4;
+    const struct {
+        const char *name;
+        const void *p;
+        size_t bytes, align;
+    } args[] = {{"want", want, rows, 4},   // the only one that is not written
+                {"table", table, cols > 0 && R > 0 ? ((size_t)(R - 1) * ld_table + cols) * 4 : 0, 4},
+                {"kv_len", kv_len, rows, 4},
+                {"free_pages", free_pages, (size_t)P * 4, 4},
+                {"free_count", free_count, 4, 4},
+                {"start", start, start ? rows : 0, 4},
+                {"offsets", offsets, offsets ? rows + 4 : 0, 4},
+                {"positions", positions, positions ? (size_t)N * 4 : 0, 4},
+                {"slots", slots, slots ? (size_t)N * 8 : 0, 8},
+                {"workspace", workspace, need, 16}};
+    for (const auto &x : args)
+        if (!aligned(x.p, x.align)) return fail(FS_ERR_INVALID_ARG, "%s must be %zu-byte aligned", x.name, x.align);
+    for (size_t i = 1; i < sizeof args / sizeof *args; ++i)
+        for (size_t j = 0; j < i; ++j)
+            if (overlaps(args[i].p, args[i].bytes, args[j].p, args[j].bytes))
+                return fail(FS_ERR_INVALID_ARG, "%s overlaps %s", args[i].name, args[j].name);
+    fs::PagedResize a{table, ld_table, cols, kv_len, want, R, page, free_pages, free_count, P, start, offsets, positions, slots, N,
+                      static_cast<unsigned char *>(workspace)};
+    hipError_t e = fs::launch_paged_resize(a, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "fs_paged_resize launch");
+    return FS_OK;
+}
+
+int fs_rotary_frequencies(double *freq, int rot, double base, double factor, int context, double fast, double slow)
+{
+    g_last_error.clear();
+    if (rot < 0 || rot % 2) return fail(FS_ERR_INVALID_ARG, "rot=%d is not an even number", rot);
+    const double most = std::numeric_limits<double>::max();
+    if (!(base > 0 && base <= most) || !(factor > 0 && factor <= most))
+        return fail(FS_ERR_INVALID_ARG, "base=%g and factor=%g must be positive and finite", base, factor);
+    if (context < 0) return fail(FS_ERR_INVALID_ARG, "context=%d < 0", context);
+    if (context > 0 && !(slow >= 0 && fast > slow && fast <= most))
+        return fail(FS_ERR_INVALID_ARG, "fast=%g must be above slow=%g, both finite and not negative", fast, slow);
+    if (rot == 0) return FS_OK;
+    if (!freq) return fail(FS_ERR_INVALID_ARG, "null pointer (freq)");
+    for (int i = 0; i < rot / 2; ++i) {
+        const double f = std::pow(base, -2.0 * i / rot);
+        double keep = 0;
+        if (context > 0) keep = std::min(1.0, std::max(0.0, (context * f / (2 * 3.14159265358979323846) - slow) / (fast - slow)));
+        freq[i] = f / factor * (1 - keep) + f * keep;
+    }
+    return FS_OK;
+}
+
+int fs_rotary(const void *q, int64_t q_token_stride, int64_t q_head_stride, const void *k, int64_t k_token_stride,
+              int64_t k_head_stride, const int32_t *positions, const double *freq, int rot, int interleaved, float magnitude,
+              void *q_out, int64_t q_out_token_stride, int64_t q_out_head_stride, void *k_out, int64_t k_out_token_stride,
+              int64_t k_out_head_stride, int N, int Hq, int Hkv, int D, int dtype, void *stream)
+{
+    g_last_error.clear();
+    if (N < 0 || Hq < 0 || Hkv < 0 || D < 0)
+        return fail(FS_ERR_INVALID_ARG, "negative size (N=%d Hq=%d Hkv=%d D=%d)", N, Hq, Hkv, D);
+    if (dtype != FS_F32 && dtype != FS_BF16) return fail(FS_ERR_UNSUPPORTED, "dtype %d is not FS_F32 or FS_BF16", dtype);
+    if (!supported_d(D)) return fail(FS_ERR_UNSUPPORTED, "head dim D=%d not in {16,32,64,128}", D);
+    if (rot < 0 || rot % 2 || rot > D) return fail(FS_ERR_INVALID_ARG, "rot=%d is not an even number of at most D=%d", rot, D);
+    if (interleaved != 0 && interleaved != 1) return fail(FS_ERR_INVALID_ARG, "interleaved=%d is neither 0 nor 1", interleaved);
+    if ((long long)Hq + Hkv > (1 << 17)) return fail(FS_ERR_UNSUPPORTED, "Hq=%d and Hkv=%d are more than 2^17 heads", Hq, Hkv);
+    if (N == 0 || (Hq == 0 && Hkv == 0)) return FS_OK;
+    if ((Hq > 0 && (!q || !q_out)) || (Hkv > 0 && (!k || !k_out)) || !positions || (rot > 0 && !freq))
+        return fail(FS_ERR_INVALID_ARG, "null pointer (q=%p q_out=%p k=%p k_out=%p positions=%p freq=%p)", q, q_out, k, k_out,
+                    (const void *)positions, (const void *)freq);
+    if (!aligned(positions, 4) || !aligned(freq, 8)) return fail(FS_ERR_INVALID_ARG, "positions and freq must be aligned to their elements");
+    const long long e = dtype == FS_BF16 ? 2 : 4;
+    const int64_t per16 = 16 / e;
+    struct {
+        const void *p;
+        int64_t token, head;
+        int H;
+        bool written;
+        Tokens x;
+    } t[4] = {{q, q_token_stride, q_head_stride, Hq, false, {}}, {k, k_token_stride, k_head_stride, Hkv, false, {}},
+              {q_out, q_out_token_stride, q_out_head_stride, Hq, true, {}}, {k_out, k_out_token_stride, k_out_head_stride, Hkv, true, {}}};
+    for (auto &y : t) {
+        if (y.H == 0) continue;
+        if (!aligned(y.p, 16)) return fail(FS_ERR_INVALID_ARG, "q, k and the outputs must be 16-byte aligned");
+        if (y.token < 0 || y.head < 0) return fail(FS_ERR_INVALID_ARG, "negative stride of q, k or an output");
+        if ((N > 1 && y.token % per16) || (y.H > 1 && y.head % per16))
+            return fail(FS_ERR_INVALID_ARG, "the strides of q, k and the outputs must be multiples of 16 bytes");
+        const long long bytes = extent(N, y.token, y.H, y.head, 1, 0, D, (size_t)e);
+        if (bytes < 0) return fail(FS_ERR_UNSUPPORTED, "the strides of q, k and the outputs are too large");
+        if (y.written && !rows_apart(N, y.token, y.H, y.head, D))
+            return fail(FS_ERR_INVALID_ARG, "rows of an output lie on one another");
+        y.x = Tokens{y.p, N > 1 ? y.token * e : 0, y.H > 1 ? y.head * e : 0, (long long)D * e, bytes, y.H};
+    }
+    for (int o = 2; o < 4; ++o) {
+        if (t[o].H == 0) continue;
+        if (overlaps(t[o].p, (size_t)t[o].x.bytes, positions, (size_t)N * 4) ||
+            overlaps(t[o].p, (size_t)t[o].x.bytes, freq, (size_t)(rot / 2) * 8))
+            return fail(FS_ERR_INVALID_ARG, "an output overlaps positions or freq");
+        for (int i = 0; i < o; ++i) {
+            if (t[i].H == 0) continue;
+            // in place: the very same rows
+            if (i == o - 2 && t[i].p == t[o].p && t[i].x.token == t[o].x.token && t[i].x.head == t[o].x.head) continue;
+            if (tokens_meet(t[i].x, t[o].x, N)) return fail(FS_ERR_INVALID_ARG, "an output overlaps q, k or the other output");
+        }
+    }
+    auto rows = [&](int i) {
+        return fs::RotaryRows{static_cast<const unsigned char *>(t[i].p), static_cast<unsigned char *>(const_cast<void *>(t[i + 2].p)),
+                              t[i].x.token, t[i].x.head, t[i + 2].x.token, t[i + 2].x.head};
+    };
+    fs::Rotary a{rows(0), rows(1), positions, freq, rot, N, Hq, Hkv, magnitude};
+    hipError_t err = fs::launch_rotary(a, D, dtype == FS_BF16, interleaved == 1, static_cast<hipStream_t>(stream));
+    if (err != hipSuccess) return hip_fail(err, "fs_rotary launch");
+    return FS_OK;
+}
+
+size_t fs_paged_chunk_attn_workspace_bytes(int N, int R, int Hq, int Hkv, int page, int cols, int D, int dtype) {
+    g_last_error.clear();
+    if (check_chunk_sizes(N, R, Hq, Hkv, page, cols, D, dtype) != FS_OK) return (size_t)-1;
+    if (N == 0 || R == 0 || Hq == 0) return 0;
+    return fs::paged_chunk_attn_workspace_bytes(N, R, Hq, Hkv, page, cols, D, dtype == FS_BF16);
+}
+
+int fs_paged_chunk_attn(const void *q, int64_t q_token_stride, int64_t q_head_stride, const void *K, const void *V,
+                        int64_t page_stride, int64_t head_stride, int64_t slot_stride, int P, int page, const int32_t *table,
+                        int ld_table, int cols, const int32_t *kv_len, const int32_t *offsets, float scale, void *out, int N, int R,
+                        int Hq, int Hkv, int D, int dtype, void *workspace, size_t workspace_bytes, void *stream)
+{
+    g_last_error.clear();
+    int st = check_paged_sizes(R, Hkv, P, page, ld_table, cols, D, dtype);
+    if (st != FS_OK) return st;
+    if ((st = check_chunk_sizes(N, R, Hq, Hkv, page, cols, D, dtype)) != FS_OK) return st;
+    const float base2 = scale * 1.44269504f;   // what the scores are multiplied with
+    if (!(base2 > -std::numeric_limits<float>::infinity() && base2 < std::numeric_limits<float>::infinity()))
+        return fail(FS_ERR_INVALID_ARG, "scale * log2(e) is not finite");
+    if (N == 0 || R == 0 || Hq == 0) return FS_OK;
+    const size_t esize = dtype == FS_BF16 ? 2 : 4;
+    size_t kv_bytes = 0, table_bytes = 0;
+    if ((st = check_paged(K, V, page_stride, head_stride, slot_stride, P, page, table, ld_table, cols, R, Hkv, D, dtype,
+                          &kv_bytes, &table_bytes)) != FS_OK)
+        return st;
+    if (!q || !out || !kv_len || !offsets)
+        return fail(FS_ERR_INVALID_ARG, "null pointer (q=%p out=%p kv_len=%p offsets=%p)", q, out, (const void *)kv_len,
+                    (const void *)offsets);
+    if (!aligned(q, 16) || !aligned(out, 16)) return fail(FS_ERR_INVALID_ARG, "q and out must be 16-byte aligned");
+    if (!aligned(kv_len, 4) || !aligned(offsets, 4)) return fail(FS_ERR_INVALID_ARG, "kv_len and offsets must be 4-byte aligned");
+    if (q_token_stride < 0 || q_head_stride < 0) return fail(FS_ERR_INVALID_ARG, "negative stride of q");
+    const int64_t per16 = (int64_t)(16 / esize);
+    if ((N > 1 && q_token_stride % per16) || (Hq > 1 && q_head_stride % per16))
+        return fail(FS_ERR_INVALID_ARG, "the strides of q must be multiples of 16 bytes");
+    const long long q_bytes = extent(N, q_token_stride, Hq, q_head_stride, 1, 0, D, esize);
+    if (q_bytes < 0) return fail(FS_ERR_UNSUPPORTED, "the strides of q are too large");
+    const size_t out_bytes = (size_t)N * Hq * D * esize, rows = (size_t)R * 4;
+    const size_t need = fs::paged_chunk_attn_workspace_bytes(N, R, Hq, Hkv, page, cols, D, dtype == FS_BF16);
+    if (workspace_bytes < need || !workspace)
+        return fail(FS_ERR_INVALID_ARG, "workspace of %zu bytes at %p; %zu bytes needed", workspace_bytes, workspace, need);
+    if (!aligned(workspace, 16)) return fail(FS_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
+    const struct {
+        const void *p;
+        size_t bytes;
+    } inputs[] = {{q, (size_t)q_bytes}, {K, kv_bytes}, {V, kv_bytes}, {table, table_bytes}, {kv_len, rows}, {offsets, rows + 4}};
+    for (const auto &x : inputs) {
+        if (overlaps(out, out_bytes, x.p, x.bytes)) return fail(FS_ERR_INVALID_ARG, "out overlaps an input");
+        if (overlaps(workspace, need, x.p, x.bytes)) return fail(FS_ERR_INVALID_ARG, "workspace overlaps an argument");
+    }
+    if (overlaps(workspace, need, out, out_bytes)) return fail(FS_ERR_INVALID_ARG, "workspace overlaps an argument");
+
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (validate_mode() && (st = validate_lengths(kv_len, R, cols * page, s, "kv_len")) != FS_OK) return st;
+    fs::PagedChunk a{};
+    a.cache = paged_cache(const_cast<void *>(K), const_cast<void *>(V), page_stride, head_stride, slot_stride, P, page, table,
+                          ld_table, cols, esize);
+    const long long e = (long long)esize;
+    a.q = static_cast<const unsigned char *>(q), a.q_token_bytes = q_token_stride * e, a.q_head_bytes = q_head_stride * e;
+    a.kv_len = kv_len, a.offsets = offsets;
+    a.out = static_cast<unsigned char *>(out);
+    a.N = N, a.R = R, a.Hq = Hq, a.Hkv = Hkv, a.scale = scale;
+    a.workspace = static_cast<unsigned char *>(workspace);
+    hipError_t err = fs::launch_paged_chunk_attn(a, D, dtype == FS_BF16, s);
+    if (err != hipSuccess) return hip_fail(err, "fs_paged_chunk_attn launch");
     return FS_OK;
 }
 

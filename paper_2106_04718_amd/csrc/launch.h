@@ -143,6 +143,54 @@ struct PagedAttn {
 size_t paged_attn_workspace_bytes(int R, int Hq, int Hkv, int page, int cols, int D);
 hipError_t launch_paged_attn(const PagedAttn &a, int D, bool bf16, hipStream_t stream);
 
+// Rows of a paged cache grow and shrink: kv_len [R] becomes want [R], pages go back
+// to the stack free_pages [pages] of *free_count and come from it, and the tokens added
+// get their positions and slots (N entries each; null: not asked for).
+struct PagedResize {
+    int32_t *table;
+    int ld_table, cols;
+    int32_t *kv_len;
+    const int32_t *want;
+    int R, page;
+    int32_t *free_pages, *free_count;
+    int pages;
+    int32_t *start, *offsets, *positions;   // each may be null
+    int64_t *slots;
+    int N;
+    unsigned char *workspace;
+};
+size_t paged_resize_workspace_bytes(int R);
+hipError_t launch_paged_resize(const PagedResize &a, hipStream_t stream);
+
+// Rotary positions: N tokens of Hq and Hkv heads, read and written (strides in bytes).
+struct RotaryRows {
+    const unsigned char *from;
+    unsigned char *to;
+    long long from_token, from_head, to_token, to_head;
+};
+struct Rotary {
+    RotaryRows q, k;
+    const int32_t *positions;
+    const double *freq;   // [rot / 2]
+    int rot, N, Hq, Hkv;
+    float magnitude;
+};
+hipError_t launch_rotary(const Rotary &a, int D, bool bf16, bool interleaved, hipStream_t stream);
+
+// Attention of the last offsets[r + 1] - offsets[r] positions of each row, causal.
+struct PagedChunk {
+    PagedCache cache;
+    const unsigned char *q;   // [N, Hq, D]
+    long long q_token_bytes, q_head_bytes;
+    const int32_t *kv_len, *offsets;
+    unsigned char *out;       // [N, Hq, D], contiguous
+    int N, R, Hq, Hkv;
+    float scale;
+    unsigned char *workspace;
+};
+size_t paged_chunk_attn_workspace_bytes(int N, int R, int Hq, int Hkv, int page, int cols, int D, bool bf16);
+hipError_t launch_paged_chunk_attn(const PagedChunk &a, int D, bool bf16, hipStream_t stream);
+
 // One token per row of logits [R, V] (leading dimension ld).  A null parameter
 // array means that its filter is off.
 struct TokenSample {

@@ -154,6 +154,48 @@ static PyObject *py_paged_attn(PyObject *self, PyObject *const *args, Py_ssize_t
     return PyLong_FromLong(st);
 }
 
+static PyObject *py_paged_resize(PyObject *self, PyObject *const *args, Py_ssize_t nargs) {
+    unsigned long long u[18];
+    int v[18];
+    (void)self;
+    if (unpack(args, nargs, "piippiippippppippp", u, v)) return NULL;
+    int st = fs_paged_resize((int32_t *)PTR(0), v[1], v[2], (int32_t *)PTR(3), (const int32_t *)PTR(4), v[5], v[6],
+                             (int32_t *)PTR(7), (int32_t *)PTR(8), v[9], (int32_t *)PTR(10), (int32_t *)PTR(11),
+                             (int32_t *)PTR(12), (int64_t *)PTR(13), v[14], PTR(15), (size_t)u[16], PTR(17));
+    return PyLong_FromLong(st);
+}
+
+/* magnitude, a C float, is passed after the arguments that unpack() takes */
+static PyObject *py_rotary(PyObject *self, PyObject *const *args, Py_ssize_t nargs) {
+    unsigned long long u[22];
+    int v[22];
+    (void)self;
+    if (nargs != 23) return PyErr_Format(PyExc_TypeError, "expected 23 arguments, got %zd", nargs);
+    if (unpack(args, 22, "ppppppppii" "pppppp" "iiiii" "p", u, v)) return NULL;
+    const double magnitude = PyFloat_AsDouble(args[22]);
+    if (PyErr_Occurred()) return NULL;
+    int st = fs_rotary(PTR(0), (int64_t)u[1], (int64_t)u[2], PTR(3), (int64_t)u[4], (int64_t)u[5], (const int32_t *)PTR(6),
+                       (const double *)PTR(7), v[8], v[9], (float)magnitude, PTR(10), (int64_t)u[11], (int64_t)u[12], PTR(13),
+                       (int64_t)u[14], (int64_t)u[15], v[16], v[17], v[18], v[19], v[20], PTR(21));
+    return PyLong_FromLong(st);
+}
+
+/* scale, a C float, is passed after the arguments that unpack() takes */
+static PyObject *py_paged_chunk_attn(PyObject *self, PyObject *const *args, Py_ssize_t nargs) {
+    unsigned long long u[25];
+    int v[25];
+    (void)self;
+    if (nargs != 26) return PyErr_Format(PyExc_TypeError, "expected 26 arguments, got %zd", nargs);
+    if (unpack(args, 25, "ppppppppiipiippp" "iiiiii" "ppp", u, v)) return NULL;
+    const double scale = PyFloat_AsDouble(args[25]);
+    if (PyErr_Occurred()) return NULL;
+    int st = fs_paged_chunk_attn(PTR(0), (int64_t)u[1], (int64_t)u[2], PTR(3), PTR(4), (int64_t)u[5], (int64_t)u[6],
+                                 (int64_t)u[7], v[8], v[9], (const int32_t *)PTR(10), v[11], v[12], (const int32_t *)PTR(13),
+                                 (const int32_t *)PTR(14), (float)scale, PTR(15), v[16], v[17], v[18], v[19], v[20], v[21],
+                                 PTR(22), (size_t)u[23], PTR(24));
+    return PyLong_FromLong(st);
+}
+
 static PyObject *py_token_sample(PyObject *self, PyObject *const *args, Py_ssize_t nargs) {
     unsigned long long u[15];
     int v[15];
@@ -199,6 +241,16 @@ static PyMethodDef methods[] = {
      "fs_paged_attn(q, q_row_stride, q_head_stride, K, V, page_stride, head_stride, slot_stride, P, page, table, "
      "ld_table, cols, kv_len, k, v, new_row_stride, new_head_stride, out, R, Hq, Hkv, D, dtype, workspace, "
      "workspace_bytes, stream, scale)"},
+    {"fs_paged_resize", (PyCFunction)(void (*)(void))py_paged_resize, METH_FASTCALL,
+     "fs_paged_resize(table, ld_table, cols, kv_len, want, R, page, free_pages, free_count, P, start, offsets, positions, "
+     "slots, N, workspace, workspace_bytes, stream)"},
+    {"fs_rotary", (PyCFunction)(void (*)(void))py_rotary, METH_FASTCALL,
+     "fs_rotary(q, q_token_stride, q_head_stride, k, k_token_stride, k_head_stride, positions, freq, rot, interleaved, "
+     "q_out, q_out_token_stride, q_out_head_stride, k_out, k_out_token_stride, k_out_head_stride, N, Hq, Hkv, D, dtype, "
+     "stream, magnitude)"},
+    {"fs_paged_chunk_attn", (PyCFunction)(void (*)(void))py_paged_chunk_attn, METH_FASTCALL,
+     "fs_paged_chunk_attn(q, q_token_stride, q_head_stride, K, V, page_stride, head_stride, slot_stride, P, page, table, "
+     "ld_table, cols, kv_len, offsets, out, N, R, Hq, Hkv, D, dtype, workspace, workspace_bytes, stream, scale)"},
     {"fs_token_sample", (PyCFunction)(void (*)(void))py_token_sample, METH_FASTCALL,
      "fs_token_sample(logits, ld_logits, R, V, dtype, u, temperature, top_k, top_p, min_p, out_token, out_logprob, "
      "workspace, workspace_bytes, stream)"},

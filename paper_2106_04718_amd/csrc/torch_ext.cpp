@@ -355,6 +355,84 @@ PyObject *paged_attn(PyObject *, PyObject *const *a, Py_ssize_t n) {
         (int)q.size(1), (int)K.size(1), (int)K.size(3), code(K.scalar_type()), ws.data_ptr(), ws.nbytes(), s));
 }
 
+// paged_resize(table, kv_len, want, free_pages, free_count, page, start, offsets, positions, slots (each or None), workspace)
+PyObject *paged_resize(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    if (n != 11) return declined();
+    Args g{a};
+    const at::Tensor &tb = *g.tensor(0), &len = *g.tensor(1), &want = *g.tensor(2), &fp = *g.tensor(3), &fc = *g.tensor(4),
+                     &ws = *g.tensor(10);
+    const long long page = g.integer(5);
+    const at::Tensor *start = optional(g, 6), *off = optional(g, 7), *pos = optional(g, 8), *slots = optional(g, 9);
+    int ld = 0;
+    void *s = nullptr;
+    if (!g.ok || tb.dim() != 2 || !table(tb, tb.size(0), ld) || !fits(tb.size(0)) || !ints(len, tb.size(0)) ||
+        !ints(want, tb.size(0)) || fp.dim() != 1 || !ints(fp, fp.size(0)) || !fits(fp.size(0)) || !ints(fc, 1) ||
+        !ws.is_contiguous() || (start && !ints(*start, tb.size(0))) || (off && !ints(*off, tb.size(0) + 1)))
+        return declined();
+    int64_t N = 0;
+    if (pos) {
+        if (pos->dim() != 1 || !ints(*pos, pos->size(0))) return declined();
+        N = pos->size(0);
+    }
+    if (slots) {
+        if (slots->dim() != 1 || slots->scalar_type() != at::kLong || !slots->is_contiguous() || (pos && slots->size(0) != N))
+            return declined();
+        N = slots->size(0);
+    }
+    if (!fits(N) || !stream_of(g, s)) return declined();
+    return PyLong_FromLong(fs_paged_resize(
+        data<int32_t>(&tb), ld, (int)tb.size(1), data<int32_t>(&len), data<int32_t>(&want), (int)tb.size(0), (int)page,
+        data<int32_t>(&fp), data<int32_t>(&fc), (int)fp.size(0), data<int32_t>(start), data<int32_t>(off), data<int32_t>(pos),
+        data<int64_t>(slots), (int)N, ws.data_ptr(), ws.nbytes(), s));
+}
+
+// rotary(q, positions, freq, k or None, interleaved, magnitude, out, k_out or None)
+PyObject *rotary(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    if (n != 8) return declined();
+    Args g{a};
+    const at::Tensor &q = *g.tensor(0), &pos = *g.tensor(1), &freq = *g.tensor(2), &out = *g.tensor(6);
+    const at::Tensor *k = optional(g, 3), *k_out = optional(g, 7);
+    void *s = nullptr;
+    if (!g.ok || !PyBool_Check(a[4]) || !PyFloat_CheckExact(a[5]) || q.dim() != 3 || code(q.scalar_type()) < 0 || !k != !k_out)
+        return declined();
+    const at::ScalarType ty = q.scalar_type();
+    if (!rows_of(q, 3, ty) || !all_fit(q) || !rows_of(out, 3, ty) || out.sizes() != q.sizes() || !ints(pos, q.size(0)) ||
+        freq.scalar_type() != at::kDouble || freq.dim() != 1 || !freq.is_contiguous() || freq.size(0) > INT_MAX / 2)
+        return declined();
+    if (k && (!rows_of(*k, 3, ty) || !all_fit(*k) || !rows_of(*k_out, 3, ty) || k_out->sizes() != k->sizes() ||
+              k->size(0) != q.size(0) || k->size(2) != q.size(2)))
+        return declined();
+    if (!stream_of(g, s)) return declined();
+    return PyLong_FromLong(fs_rotary(
+        q.data_ptr(), q.stride(0), q.stride(1), data<void>(k), k ? k->stride(0) : 0, k ? k->stride(1) : 0, data<int32_t>(&pos),
+        data<double>(&freq), 2 * (int)freq.size(0), a[4] == Py_True, (float)PyFloat_AS_DOUBLE(a[5]), out.data_ptr(), out.stride(0),
+        out.stride(1), data<void>(k_out), k ? k_out->stride(0) : 0, k ? k_out->stride(1) : 0, (int)q.size(0), (int)q.size(1),
+        k ? (int)k->size(1) : 0, (int)q.size(2), code(ty), s));
+}
+
+// paged_chunk_attn(q, K, V, table, kv_len, offsets, out, workspace, scale or None)
+PyObject *paged_chunk_attn(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    if (n != 9) return declined();
+    Args g{a};
+    const at::Tensor &q = *g.tensor(0), &K = *g.tensor(1), &V = *g.tensor(2), &tb = *g.tensor(3), &len = *g.tensor(4),
+                     &off = *g.tensor(5), &out = *g.tensor(6), &ws = *g.tensor(7);
+    int ld = 0;
+    void *s = nullptr;
+    if (!g.ok || !paged(K, V, tb, ld) || !rows_of(q, 3, K.scalar_type()) || !all_fit(q) || q.size(2) != K.size(3) ||
+        !ints(len, tb.size(0)) || !ints(off, tb.size(0) + 1) || !same(out, q) || !out.is_contiguous() || !ws.is_contiguous())
+        return declined();
+    double scale = 0;
+    if (a[8] == Py_None) scale = K.size(3) ? std::pow((double)K.size(3), -0.5) : 1.0;
+    else if (PyFloat_CheckExact(a[8])) scale = PyFloat_AS_DOUBLE(a[8]);
+    else return declined();
+    if (!stream_of(g, s)) return declined();
+    return PyLong_FromLong(fs_paged_chunk_attn(
+        q.data_ptr(), q.stride(0), q.stride(1), K.data_ptr(), V.data_ptr(), K.stride(0), K.stride(1), K.stride(2),
+        (int)K.size(0), (int)K.size(2), data<int32_t>(&tb), ld, (int)tb.size(1), data<int32_t>(&len), data<int32_t>(&off),
+        (float)scale, out.data_ptr(), (int)q.size(0), (int)tb.size(0), (int)q.size(1), (int)K.size(1), (int)K.size(3),
+        code(K.scalar_type()), ws.data_ptr(), ws.nbytes(), s));
+}
+
 // token_sample(logits, u, temperature, top_k, top_p, min_p (each or None), token, logprob, workspace)
 PyObject *token_sample(PyObject *, PyObject *const *a, Py_ssize_t n) {
     if (n != 9) return declined();
@@ -402,6 +480,10 @@ PyMethodDef methods[] = {
     {"ancestry_step", FS_FAST(ancestry_step), "(anc, parent, k, t)"},
     {"paged_append", FS_FAST(paged_append), "(K, V, k, v, table, start, offsets or None)"},
     {"paged_attn", FS_FAST(paged_attn), "(q, K, V, table, kv_len, out, workspace, k or None, v or None, scale or None)"},
+    {"paged_resize", FS_FAST(paged_resize),
+     "(table, kv_len, want, free_pages, free_count, page, start, offsets, positions, slots, workspace), outputs None: not made"},
+    {"rotary", FS_FAST(rotary), "(q, positions, freq, k or None, interleaved, magnitude, out, k_out or None)"},
+    {"paged_chunk_attn", FS_FAST(paged_chunk_attn), "(q, K, V, table, kv_len, offsets, out, workspace, scale or None)"},
     {"token_sample", FS_FAST(token_sample),
      "(logits, u, temperature, top_k, top_p, min_p, token, logprob, workspace), settings None: off"},
     {nullptr, nullptr, 0, nullptr},
