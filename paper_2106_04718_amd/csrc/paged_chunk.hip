@@ -8,12 +8,13 @@
 // paged_tile.h describes, its four waves the positions in turn; their softmax states are
 // joined at the end.
 //
-// Division of the work.  The columns of a row are cut into tiles, and a tile's positions, in
-// units of 128, into as many chunks as the tiles leave room on the chip for.  Lengths are
-// known on the device alone, so every workgroup adds the rows' work up and finds its own
-// piece (up to kScanRows rows; above, a kernel before this one does it for all).  A tile of
-// one chunk is written at once; the chunks of the others leave their softmax states in the
-// workspace, and the last of them to arrive joins them, in the order of the chunks.
+// Division of the work.  The columns of a row are cut into tiles.  Either workgroups take whole
+// tiles, the longest first; or all tiles of a key-value head, one behind another, are cut into
+// as many equal shares as the head has of the workgroups that fit the chip.  A share may begin
+// and end within a tile, at a unit of 128 positions; the tile's parts then leave their softmax
+// states in the workspace, where the last of them to arrive joins them, in their order.
+// Lengths are known on the device alone, so every workgroup adds the rows' work up and finds
+// its own (up to kScanRows rows; above, a kernel before this one adds up, and the work is cut).
 #include <math.h>
 #include <stdint.h>
 
@@ -27,10 +28,11 @@
 namespace fs {
 namespace {
 
-constexpr int kPlaces = 512;      // workgroups that fit the 256 CUs at once, two each
-constexpr int kChunks = 2 * kPlaces;   // chunks that the work is cut into at most, but for one begun per tile
+constexpr int kMostShares = 4 * 1024;   // of all heads together
 constexpr int kJoin = 64;         // states joined at a time
 constexpr int kScanRows = 256;    // rows whose lengths every workgroup looks at: four a lane
+constexpr int kStart = 128;       // what a tile takes beside its positions, in positions
+constexpr int kLeast = 512;       // a share at least
 
 constexpr int kWideTile = 64;     // positions that a workgroup attends at a time in a wide tile
 constexpr int kWideColumns = 32 * kWaves;
@@ -46,173 +48,217 @@ typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
 constexpr int kSchedValu = 0x2, kSchedMfma = 0x8, kSchedRead = 0x100;   // kinds of instructions
 
+typedef unsigned long long u64_t;
+
 // What a launch knows beside PagedChunk.
 struct Geo {
     Div by_page, by_hkv, by_g;
     int G;
-    int narrow, wide;          // columns of a tile of a row of up to `narrow` columns, and of others
+    int width;                 // columns of a tile: a power of two
+    double half;               // half of the tokens of a tile
     unsigned page16, slot16;   // strides in units of 16 bytes
-    int record;                // floats of a chunk's state: wide * (D + 2)
+    int shares;                // of a key-value head
+    int record;                // floats of a part's state: width * (D + 2)
     unsigned *group_count, *tile_count;   // arrivals, by the first record of the group or tile
-    const int4 *plan;          // made before the launch (more than kScanRows rows), or null
+    const u64_t *plan;         // work before each row and of all, made before the launch (more than kScanRows rows), or null
     float *records;
-    long long slots;           // records that there are
 };
 
-// A row's part of the work.
 struct Row {
     int first_pos;   // of its first token; may be negative, then that token attends nothing
-    int begin, columns;   // first token, and columns (of one key-value head)
-    int width, tiles;     // columns of a tile
-    int units;            // of its last tile, the longest
-};
-
-// A piece of it: units [split * c, split * c + c) of tile `tile` of row r; the records of the
-// tile's chunks begin at `slot`.
-struct Task {
-    int r, tile, split, splits, slot;
+    int begin, tokens;
+    int columns, tiles;   // of one key-value head
 };
 
 __device__ __forceinline__ int units_of(int L) { return L <= 0 ? 1 : (L + kUnit - 1) / kUnit; }
 
 __device__ __forceinline__ Row row_of(const PagedChunk &a, const Geo &geo, int kv_len, int o0, int o1) {
-    const int cap = a.cache.cols * a.cache.page;
     o0 = o0 < 0 ? 0 : o0, o1 = o1 < a.N ? o1 : a.N;   // of tokens that there are
     const int n = o1 > o0 ? o1 - o0 : 0, L = kv_len < 0 ? 0 : kv_len;
     Row w;
     w.first_pos = L - n;
-    w.begin = o0;
+    w.begin = o0, w.tokens = n;
     w.columns = n * geo.G;
-    w.width = w.columns <= geo.narrow ? geo.narrow : geo.wide;   // powers of two
-    w.tiles = (int)(((unsigned)w.columns + w.width - 1) >> (31 - __builtin_clz(w.width)));
-    w.units = units_of(L < cap ? L : cap);
+    w.tiles = (int)(((unsigned)w.columns + geo.width - 1) >> (31 - __builtin_clz(geo.width)));
     return w;
 }
 
-// Units of a tile that begins and ends at these columns, and units per chunk for work of
-// `units` (tiles of a head times their units) in all.
-__device__ __forceinline__ int units_per_chunk(unsigned long long units, int heads) {
-    const unsigned long long c = (units * heads + kChunks - 1) / kChunks;
-    return c < 1 ? 1 : c > (1 << 24) ? 1 << 24 : (int)c;
-}
-__device__ __forceinline__ int splits_of(const Row &w, int c) { return (w.units + c - 1) / c; }
-
-// Sum over the lanes of values below 2^60.
-__device__ __forceinline__ unsigned long long wave_sum64(unsigned long long x) {
-    const unsigned long long a = (unsigned)wave_sum((int)(x & 0xfffff)), b = (unsigned)wave_sum((int)(x >> 20 & 0xfffff)),
-                             c = (unsigned)wave_sum((int)(x >> 40));
-    return a + (b << 20) + (c << 40);
+// Work of a row's tiles before tile i, in positions: those that a tile's last token attends, and
+// kStart.  Rising with i.  Where the tiles differ by little they count alike, so that shares
+// of a tile or a whole part of one begin together, and its neighbours find their keys in the L2.
+__device__ __forceinline__ u64_t work_before(const PagedChunk &a, const Geo &geo, const Row &w, int i) {
+    const int cap = a.cache.cols * a.cache.page, p = w.first_pos < 0 ? 0 : w.first_pos < cap ? w.first_pos : cap;
+    if (p / 2 >= w.tokens) return (u64_t)(unsigned)i * (unsigned)(p + w.tokens / 2 + kStart);
+    return (u64_t)(unsigned)i * (unsigned)(p + kStart) + (u64_t)((double)i * (double)(i + 1) * geo.half);
 }
 
-// The t-th task of up to kScanRows rows; false: there are fewer.
-__device__ __forceinline__ bool find_task(const PagedChunk &a, const Geo &geo, int t, Task &out) {
-    const int lane = (int)threadIdx.x & 63;
+__device__ __forceinline__ u64_t shfl_up64(u64_t x, int by) {
+    const unsigned lo = __shfl_up((unsigned)x, by), hi = __shfl_up((unsigned)(x >> 32), by);
+    return (u64_t)hi << 32 | lo;
+}
+__device__ __forceinline__ u64_t wave_scan64(u64_t x) {
+#pragma unroll
+    for (int by = 1; by < kWave; by *= 2) {
+        const u64_t y = shfl_up64(x, by);
+        if ((int)(threadIdx.x & 63) >= by) x += y;
+    }
+    return x;
+}
+__device__ __forceinline__ u64_t uniform64(u64_t x) {
+    return (u64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)x);
+}
+
+// What a workgroup knows of up to kScanRows rows.
+struct Rows {
+    u64_t sums[kScanRows + 1];   // work before each of them, and of all
+    int len[kScanRows], off[kScanRows + 1];
+    int longest, tiles;          // units of the longest tile, and tiles of a head
+    int row, tile;               // where tiles are taken whole: the one found
+};
+
+__device__ __forceinline__ int wave_max(int x) {
+#pragma unroll
+    for (int by = 1; by < kWave; by *= 2) {
+        const int y = __shfl_xor(x, by);
+        x = x > y ? x : y;
+    }
+    return x;
+}
+
+// Reads and adds them up, by one wave.
+__device__ __forceinline__ void add_rows(const PagedChunk &a, const Geo &geo, Rows &rows) {
+    const int lane = (int)threadIdx.x & 63, cap = a.cache.cols * a.cache.page;
     int len[4], off[5];
 #pragma unroll
     for (int i = 0; i < 4; ++i) len[i] = a.kv_len[4 * lane + i < a.R ? 4 * lane + i : a.R - 1];   // all in flight at once
 #pragma unroll
     for (int i = 0; i < 5; ++i) off[i] = a.offsets[4 * lane + i < a.R ? 4 * lane + i : a.R];
-    Row w[4];
-    unsigned long long work = 0;
+    u64_t work[4], sum = 0;
+    int longest = 0, tiles = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        w[i] = row_of(a, geo, len[i], off[i], off[i + 1]);   // none behind the last row: it would begin at its end
-        work += (unsigned long long)w[i].tiles * (unsigned)w[i].units;
+        const Row w = row_of(a, geo, len[i], off[i], off[i + 1]);   // none behind the last row: it would begin at its end
+        work[i] = work_before(a, geo, w, w.tiles), sum += work[i];
+        const int u = w.tiles ? units_of(len[i] < cap ? len[i] : cap) : 0;
+        longest = longest > u ? longest : u, tiles += w.tiles;
+        rows.len[4 * lane + i] = len[i], rows.off[4 * lane + i] = off[i];
     }
-    const int c = units_per_chunk(wave_sum64(work), a.Hkv);
-    int s[4], tasks = 0, records = 0;
+    u64_t at = wave_scan64(sum) - sum;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        s[i] = splits_of(w[i], c);
-        tasks += w[i].tiles * s[i];
-        records += s[i] > 1 ? w[i].tiles * s[i] : 0;
+        rows.sums[4 * lane + i] = at;
+        at += work[i];
     }
-    const int all = wave_scan(tasks), slots = wave_scan(records);
-    const unsigned long long past = __ballot(all > t);
-    if (past == 0) return false;
-    int at = all - tasks, slot = slots - records, row = 4 * lane, n = 1, m = 1, first = at, begin = slot;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int here = w[i].tiles * s[i];
-        if (at <= t && here > 0) row = 4 * lane + i, n = s[i], m = w[i].tiles, first = at, begin = slot;
-        at += here;
-        slot += s[i] > 1 ? here : 0;
-    }
-    const int owner = __ffsll((long long)past) - 1;
-    out.r = __builtin_amdgcn_readlane(row, owner);
-    out.splits = __builtin_amdgcn_readlane(n, owner);
-    const int x = t - __builtin_amdgcn_readlane(first, owner);
-    out.tile = x / out.splits;
-    out.split = x - out.tile * out.splits;
-    out.slot = __builtin_amdgcn_readlane(begin, owner) + out.tile * out.splits;
-    out.tile = __builtin_amdgcn_readlane(m, owner) - 1 - out.tile;   // the longest first
-    return true;
+    longest = wave_max(longest), tiles = wave_sum(tiles);
+    if (lane == 63) rows.sums[kScanRows] = at, rows.off[kScanRows] = off[4], rows.longest = longest, rows.tiles = tiles;
 }
 
-// For any number of rows, by one workgroup: plan[1 + r] = (tasks and records of the rows
-// before r, splits of its tiles, its tiles), plan[0] = (tasks).
-__global__ __launch_bounds__(1024) void chunk_plan_kernel(PagedChunk a, Geo geo, int4 *plan) {
-    __shared__ unsigned long long total;
-    __shared__ int part[2][16], base[2];
-    const int tid = (int)threadIdx.x, lane = tid & 63, wv = tid / kWave;
-    if (tid == 0) total = 0, base[0] = base[1] = 0;
-    __syncthreads();
-    unsigned long long mine = 0;
-    for (int r = tid; r < a.R; r += 1024) {
-        const Row w = row_of(a, geo, a.kv_len[r], a.offsets[r], a.offsets[r + 1]);
-        mine += (unsigned long long)w.tiles * (unsigned)w.units;
+// The first tile of a row with at least x units (its tiles if there is none).
+__device__ __forceinline__ int first_of(const PagedChunk &a, const Geo &geo, const Row &w, int x) {
+    if (x <= 1) return 0;   // every tile has one, if only to be written
+    if ((long long)(x - 1) * kUnit >= (long long)a.cache.cols * a.cache.page) return w.tiles;
+    const long long q = (long long)(x - 1) * kUnit - w.first_pos;   // a tile's last token has to be this one or behind
+    if (q <= 0) return 0;
+    return q * geo.G >= w.columns ? w.tiles : (int)((unsigned)(q * geo.G) >> (31 - __builtin_clz(geo.width)));
+}
+
+// The t-th tile of a head in the order of falling length, by one wave: those of at least x units
+// are counted in closed form, and x found by bisection.
+__device__ __forceinline__ void find_tile(const PagedChunk &a, const Geo &geo, Rows &rows, int t) {
+    const int lane = (int)threadIdx.x & 63;
+    Row w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = row_of(a, geo, rows.len[4 * lane + i], rows.off[4 * lane + i], rows.off[4 * lane + i + 1]);
+    auto longer = [&](int x) {
+        int m = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) m += w[i].tiles - first_of(a, geo, w[i], x);
+        return wave_sum(m);
+    };
+    int lo = 1, hi = rows.longest + 1, behind = 0;   // tiles of at least hi units
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2, m = longer(mid);
+        if (m > t) lo = mid;
+        else hi = mid, behind = m;
     }
-    atomicAdd(&total, mine);
-    __syncthreads();
-    const int c = units_per_chunk(total, a.Hkv);
+    t -= behind;
+    int here[4], sum = 0;   // of just lo units
+#pragma unroll
+    for (int i = 0; i < 4; ++i) here[i] = first_of(a, geo, w[i], lo + 1) - first_of(a, geo, w[i], lo), sum += here[i];
+    int at = wave_scan(sum) - sum;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (at <= t && t < at + here[i]) rows.row = 4 * lane + i, rows.tile = first_of(a, geo, w[i], lo) + t - at;
+        at += here[i];
+    }
+}
+
+// The work before each of any number of rows, and of all, by one workgroup.
+__global__ __launch_bounds__(1024) void chunk_plan_kernel(PagedChunk a, Geo geo, u64_t *sums) {
+    __shared__ u64_t part[16];
+    const int tid = (int)threadIdx.x, wave = tid / kWave;
+    u64_t before = 0;
     for (int r0 = 0; r0 < a.R; r0 += 1024) {
         const int r = r0 + tid;
-        Row w{};
-        if (r < a.R) w = row_of(a, geo, a.kv_len[r], a.offsets[r], a.offsets[r + 1]);
-        const int s = r < a.R ? splits_of(w, c) : 1, tasks = w.tiles * s, records = s > 1 ? tasks : 0;
-        const int x = wave_scan(tasks), y = wave_scan(records);
-        if (lane == 63) part[0][wv] = x, part[1][wv] = y;
+        u64_t work = 0;
+        if (r < a.R) {
+            const Row w = row_of(a, geo, a.kv_len[r], a.offsets[r], a.offsets[r + 1]);
+            work = work_before(a, geo, w, w.tiles);
+        }
+        const u64_t run = wave_scan64(work);
+        if ((tid & 63) == 63) part[wave] = run;
         __syncthreads();
-        int t = base[0] + x - tasks, slot = base[1] + y - records;
-        for (int i = 0; i < wv; ++i) t += part[0][i], slot += part[1][i];
-        if (r < a.R) plan[1 + r] = make_int4(t, slot, s, w.tiles);
-        __syncthreads();
-        if (tid == 1023) base[0] = t + tasks, base[1] = slot + records;
+        u64_t at = before + run - work;
+        for (int i = 0; i < 16; ++i) {
+            if (i < wave) at += part[i];
+            before += part[i];
+        }
+        if (r < a.R) sums[r] = at;
         __syncthreads();
     }
-    if (tid == 0) plan[0] = make_int4(base[0], 0, 0, 0);
+    if (tid == 0) sums[a.R] = before;
 }
 
-// The t-th task of a plan: 64 rows are looked at at a time.
-__device__ __forceinline__ bool find_planned(const int4 *plan, int R, int t, Task &out) {
-    if (t >= plan[0].x) return false;
+// The last row whose work begins at or before x, 64 looked at at a time.
+__device__ __forceinline__ int row_at(const u64_t *sums, int R, u64_t x) {
     const int lane = (int)threadIdx.x & 63;
-    int lo = 0, n = R;   // the last of rows lo .. lo + n - 1 that begins at or before t
+    int lo = 0, n = R;
     while (n > 1) {
         const int step = (n + 63) / 64, at = lane * step;
-        const bool before = at < n && plan[1 + lo + at].x <= t;
-        const int last = 63 - __clzll((long long)__ballot(before));   // lane 0 always is
-        lo += last * step;
-        n = n - last * step < step ? n - last * step : step;
+        const bool there = at < n && lo + at < R;
+        const u64_t v = sums[there ? lo + at : 0];
+        lo += step * (63 - __clzll((long long)__ballot(lane == 0 || (there && v <= x))));
+        n = step;
     }
-    const int4 x = plan[1 + lo];
-    out.r = lo, out.splits = x.z;
-    const int i = t - x.x;
-    out.tile = i / x.z;
-    out.split = i - out.tile * x.z;
-    out.slot = x.y + out.tile * x.z;
-    out.tile = x.w - 1 - out.tile;
-    return true;
+    return lo;
+}
+
+// The tile of a row in which x lies, x behind the row's beginning by less than its work.
+__device__ __forceinline__ int tile_at(const PagedChunk &a, const Geo &geo, const Row &w, u64_t x) {
+    const u64_t one = work_before(a, geo, w, 1);
+    if (work_before(a, geo, w, w.tiles) == one * (unsigned)w.tiles) {   // all alike
+        const int i = (int)((double)x / (double)one);
+        return i > 0 && one * (unsigned)i > x ? i - 1 : i + 1 < w.tiles && one * (unsigned)(i + 1) <= x ? i + 1 : i;
+    }
+    const double lin = (double)one, h = geo.half;   // about h i^2 + (lin - h) i
+    const double guess = 2.0 * (double)x / ((lin - h) + sqrt((lin - h) * (lin - h) + 4.0 * h * (double)x) + 1.0);
+    int i = guess < (double)(w.tiles - 1) ? (int)guess : w.tiles - 1;
+    i = i < 0 ? 0 : i;
+    while (i > 0 && work_before(a, geo, w, i) > x) --i;
+    while (i + 1 < w.tiles && work_before(a, geo, w, i + 1) <= x) ++i;
+    return i;
 }
 
 // What a workgroup knows of its piece of work.
 struct Piece {
-    int r, h, col0, cols;     // the row, the key-value head, the tile's columns
+    int r, h, tile, col0, cols;   // the row, the key-value head, the tile and its columns
     int begin, end;           // positions of the chunk
     int seen;                 // positions that all columns attend
-    int split, splits;
+    int share, first, parts;  // the tile lies in the shares first .. first + parts - 1
     Row row;
     unsigned char *out;       // of the row and head
+    // a share has one tile that began before it, and one that began in it, which others end
+    __device__ __forceinline__ size_t record_of(const PagedChunk &a, int x) const { return (size_t)(2 * x + (x == first ? 1 : 0)) * a.Hkv + h; }
     float *record;
     // positions that a column attends: those below its limit
     __device__ __forceinline__ int limit(const PagedChunk &a, const Geo &geo, int column) const {
@@ -433,7 +479,7 @@ __device__ __forceinline__ void attend_narrow(const PagedChunk &a, const Geo &ge
     }
 
     // the four waves' states, joined, 16 columns at a time
-    const bool whole = w.splits == 1;
+    const bool whole = w.parts == 1;
 #pragma unroll
     for (int nc = 0; nc < NC; ++nc) {
         l[nc] = col_sum(l[nc]);
@@ -454,20 +500,29 @@ __device__ __forceinline__ void attend_narrow(const PagedChunk &a, const Geo &ge
                 store_out<BF16>(w.out, w.place<D>(a, geo, cc, d), ll < 0.f ? 0.f : oo / ll);
             } else {
                 put(w.record + cc * D + d, oo);
-                if (d == 0) put(w.record + geo.wide * D + 2 * cc, mm), put(w.record + geo.wide * D + 2 * cc + 1, ll);
+                if (d == 0) put(w.record + geo.width * D + 2 * cc, mm), put(w.record + geo.width * D + 2 * cc + 1, ll);
             }
         }
     }
 }
 
-// Rows of a wide tile in LDS.  With 16 bytes between them the same 16 bytes of 16 keys, and with
-// 64 (or rows of 64) the same 64 bytes of four values, lie in different banks.
+// Rows of a wide tile in LDS, as loads that go there directly leave them: 1024 bytes of a
+// wave's lanes side by side, D / 8 groups of rows; key k is row k / (D / 8) of group k % (D / 8).
+// With 16 bytes between the groups the same 16 bytes of 16 keys, and with 64 the same 64 bytes of
+// four values, lie in different banks.
 template <int D>
 struct WideLds {
-    static constexpr int kKeyRow = D * 2 + 16, kValueRow = D == 32 ? D * 2 : D * 2 + 64;
-    unsigned char k[2][kWideTile * kKeyRow], v[2][kWideTile * kValueRow];
-    unsigned bad[2];   // whether a value of the tile is infinite or NaN, where that matters
+    static constexpr int kGroups = D / 8, kKeyGroup = 1024 + 16, kValueGroup = 1024 + 64;
+    unsigned char k[2][kGroups * kKeyGroup], v[2][kGroups * kValueGroup];
+    unsigned bad;   // whether a value of the tile is infinite or NaN, where that matters
+    static __device__ __forceinline__ int value(int key) { return key % kGroups * kValueGroup + key / kGroups * (D * 2); }
 };
+
+// 16 bytes from each lane's address to LDS, a wave's side by side.
+__device__ __forceinline__ void copy16(const unsigned char *from, unsigned char *to) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from,
+                                     (__attribute__((address_space(3))) void *)to, 16, 0, 0);
+}
 
 // A lane's elements of a column, divided by its sum (negative: none), to the column's row from
 // its dim 4 h on.
@@ -488,7 +543,7 @@ __device__ __forceinline__ void write_wide(unsigned char *to, const f32x16_t (&o
 }
 
 // A tile of 128 columns, 32 a wave, over tiles of 64 positions that all four read from LDS.
-// The next tile's rows are on their way to registers meanwhile.  Lane l = 32 h + n:
+// The next tile's rows are on their way there meanwhile.  Lane l = 32 h + n:
 //   QK^T  S^T[key][column] = K . q^T, two blocks of 32 keys.  It gets the scores of column n
 //         for the keys 32 b + 8 (i / 4) + 4 h + i % 4.
 //   PV    O^T[dim][column] = V^T . P^T, contracting over 16 keys at a time in the order in which
@@ -497,8 +552,8 @@ __device__ __forceinline__ void write_wide(unsigned char *to, const f32x16_t (&o
 template <int D>
 __device__ __forceinline__ void attend_wide(const PagedChunk &a, const Geo &geo, const Piece &w, WideLds<D> &lds)
 {
-    constexpr int kPieces = D / 8, kLoads = kWideTile * kPieces / kBlock, kSteps = D / 16, kDims = D / 32;
-    constexpr int kKeyRow = WideLds<D>::kKeyRow, kValueRow = WideLds<D>::kValueRow;
+    using Lds = WideLds<D>;
+    constexpr int kGroups = Lds::kGroups, kSteps = D / 16, kDims = D / 32;
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int n = lane & 31, h = lane >> 5;
     const int begin = w.begin, end = w.end;
@@ -534,40 +589,18 @@ __device__ __forceinline__ void attend_wide(const PagedChunk &a, const Geo &geo,
         const int pg = table[geo.by_page((unsigned)(pos < end ? pos : begin))];
         return pos < end ? pg : -1;
     };
-    u32x4_t kx[kLoads], vx[kLoads];
-    unsigned long long live_next = 0;
-    auto load = [&](int t0, int pg) {
+    auto load = [&](int buf, int t0, int pg) {   // asks for a tile; which of its positions there are
         const int pos = t0 + lane;
         const bool ok = pg >= 0 && pg < c.pages;
         const unsigned off = ok ? slot16(a, geo, pg, pos) : 0u;
-        live_next = __ballot(ok);
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const int piece = tid + kBlock * i, key = piece / kPieces;
-            const size_t at = (size_t)(unsigned)__builtin_amdgcn_ds_bpermute(key << 2, (int)off) * 16 + (piece % kPieces) * 16;
-            kx[i] = *reinterpret_cast<const u32x4_t *>(Kh + at);
-            vx[i] = *reinterpret_cast<const u32x4_t *>(Vh + at);
+        for (int i = 0; i < kDims; ++i) {
+            const int g = kDims * wave + i, key = lane / kGroups * kGroups + g;
+            const size_t at = (size_t)(unsigned)__builtin_amdgcn_ds_bpermute(key << 2, (int)off) * 16 + lane % kGroups * 16;
+            copy16(Kh + at, lds.k[buf] + g * Lds::kKeyGroup);
+            copy16(Vh + at, lds.v[buf] + g * Lds::kValueGroup);
         }
-    };
-    auto stage = [&](int buf, int t0) {
-        const bool partly = t0 + kWideTile > w.seen;
-        bool bad = false;
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const int piece = tid + kBlock * i, key = piece / kPieces, c16 = (piece % kPieces) * 16;
-            if (live_next != ~0ull) {   // a position that is not there read anything
-                const uint32_t is = (live_next >> key & 1) ? 0xffffffffu : 0u;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) kx[i][j] &= is, vx[i][j] &= is;
-            }
-            if (partly) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) bad |= (vx[i][j] & 0x7f80u) == 0x7f80u || (vx[i][j] & 0x7f800000u) == 0x7f800000u;
-            }
-            *reinterpret_cast<u32x4_t *>(lds.k[buf] + key * kKeyRow + c16) = kx[i];
-            *reinterpret_cast<u32x4_t *>(lds.v[buf] + key * kValueRow + c16) = vx[i];
-        }
-        if (partly && __any(bad) && lane == 0) lds.bad[buf] = 1u;
+        return __ballot(ok);
     };
 
     f32x16_t o[kDims];
@@ -581,8 +614,8 @@ __device__ __forceinline__ void attend_wide(const PagedChunk &a, const Geo &geo,
 
     // operands: of K the lane's key n, of V^T its dim n of the keys 4 h + 0 .. 3, by a transposition
     // of the four keys that 16 lanes read
-    const unsigned char *k_at = lds.k[0] + n * kKeyRow + 16 * h;
-    const unsigned char *v_at = lds.v[0] + (4 * h + (lane & 15) / 4) * kValueRow + 32 * ((lane >> 4) & 1) + 8 * (lane & 3);
+    const unsigned char *k_at = lds.k[0] + n % kGroups * Lds::kKeyGroup + n / kGroups * (D * 2) + 16 * h;
+    const unsigned char *v_at = lds.v[0] + Lds::value(4 * h + (lane & 15) / 4) + 32 * ((lane >> 4) & 1) + 8 * (lane & 3);
     struct Values {
         bf16x8_t x[kDims];
     };
@@ -597,19 +630,19 @@ __device__ __forceinline__ void attend_wide(const PagedChunk &a, const Geo &geo,
 #pragma unroll
             for (int x = 0; x < 2; ++x)
                 v[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                    (__attribute__((address_space(3))) s16x4_t *)(at + (16 * s + 8 * x) * kValueRow + 64 * d));
+                    (__attribute__((address_space(3))) s16x4_t *)(at + Lds::value(16 * s + 8 * x) + 64 * d));
             r.x[d] = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
         }
         return r;
     };
     auto attend = [&](int buf, int t0, unsigned long long live) {
-        const unsigned char *kt = k_at + buf * (kWideTile * kKeyRow), *vt = v_at + buf * (kWideTile * kValueRow);
+        const unsigned char *kt = k_at + buf * (int)sizeof lds.k[0], *vt = v_at + buf * (int)sizeof lds.v[0];
         f32x16_t sc[2];
         bf16x8_t kf[2][kSteps];
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
 #pragma unroll
-            for (int s = 0; s < kSteps; ++s) kf[b][s] = *reinterpret_cast<const bf16x8_t *>(kt + 32 * b * kKeyRow + 32 * s);
+            for (int s = 0; s < kSteps; ++s) kf[b][s] = *reinterpret_cast<const bf16x8_t *>(kt + 32 / kGroups * b * (D * 2) + 32 * s);
         }
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
@@ -632,8 +665,17 @@ __device__ __forceinline__ void attend_wide(const PagedChunk &a, const Geo &geo,
             __builtin_amdgcn_sched_group_barrier(kSchedMfma, 1, 0);
             __builtin_amdgcn_sched_group_barrier(kSchedRead, 1, 0);
         }
-        if (t0 + kWideTile > first_lim || live != ~0ull) {
-            const int left = lim - t0;   // positions of the tile below the column's limit
+        if (live == ~0ull && t0 + kWideTile > first_lim) {
+            const int left = lim - t0 - 4 * h;   // positions of the tile below the column's limit, from the lane's first on
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (left <= 32 * b + 8 * (i / 4) + i % 4) sc[b][i] = -INFINITY;
+            }
+            any |= lim > t0;
+        } else if (live != ~0ull) {
+            const int left = lim - t0;
             const unsigned long long there = left <= 0 ? 0ull : left >= kWideTile ? live : live & ((1ull << left) - 1);
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
@@ -710,50 +752,63 @@ __device__ __forceinline__ void attend_wide(const PagedChunk &a, const Geo &geo,
         l += sum[0] + sum[1];
     };
 
-    // An infinity or NaN among the values would reach columns that do not attend its position,
-    // as 0 times it.  Such elements are added to the columns that do and taken out.
-    auto sort_out = [&](int buf, int t0) {
+    // Values of positions that are not there become zeros: the loads brought anything.  And an
+    // infinity or NaN would reach columns that do not attend its position, as 0 times it: such
+    // elements are added to the columns that do and taken out.
+    auto tidy = [&](int buf, int t0, unsigned long long live) {
+        constexpr int kMine = kWideTile * D * 2 / 16 / kBlock;   // 16-byte pieces of a lane's
+        if (tid == 0) lds.bad = 0u;
+        bool bad = false;
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) {
+            const int piece = tid + kBlock * i, key = piece / kGroups;
+            auto *x = reinterpret_cast<u32x4_t *>(lds.v[buf] + Lds::value(key) + piece % kGroups * 16);
+            if (!(live >> key & 1)) {
+                *x = u32x4_t{0u, 0u, 0u, 0u};
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) bad |= ((*x)[j] & 0x7f80u) == 0x7f80u || ((*x)[j] & 0x7f800000u) == 0x7f800000u;
+            }
+        }
+        __syncthreads();
+        if (__any(bad) && lane == 0) lds.bad = 1u;
+        __syncthreads();
+        if (!lds.bad) return;
         for (int key = 0; key < kWideTile; ++key) {
 #pragma unroll
             for (int d = 0; d < kDims; ++d) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     const int dim = 32 * d + 8 * (i / 4) + 4 * h + i % 4;
-                    const uint16_t bits = *reinterpret_cast<const uint16_t *>(lds.v[buf] + key * kValueRow + dim * 2);
-                    const float v = __uint_as_float((uint32_t)bits << 16);
+                    const float v = __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t *>(lds.v[buf] + Lds::value(key) + dim * 2) << 16);
                     if (!(fabsf(v) < INFINITY) && t0 + key < lim) o[d][i] += v;
                 }
             }
         }
         __syncthreads();
         for (int i = tid; i < kWideTile * D; i += kBlock) {
-            uint16_t *x = reinterpret_cast<uint16_t *>(lds.v[buf] + i / D * kValueRow) + i % D;
+            auto *x = reinterpret_cast<uint16_t *>(lds.v[buf] + Lds::value(i / D)) + i % D;
             if ((*x & 0x7f80u) == 0x7f80u) *x = 0;
         }
-        if (tid == 0) lds.bad[buf] = 0u;
         __syncthreads();
     };
 
     if (begin < end) {
-        if (tid < 2) lds.bad[tid] = 0u;
+        int pg = page_of(begin), buf = 0;
+        int pg_next = page_of(end - begin > kWideTile ? begin + kWideTile : begin);
+        unsigned long long live = load(0, begin, pg), live_next = 0;
+        __builtin_amdgcn_s_waitcnt(0);
         __syncthreads();
-        int pg = page_of(begin), pg_next = page_of(end - begin > kWideTile ? begin + kWideTile : begin), buf = 0;
-        load(begin, pg);
-        stage(0, begin);
-        unsigned long long live = live_next;
-        __syncthreads();
-        for (int t0 = begin;; buf ^= 1) {
+        for (int t0 = begin;; t0 += kWideTile, buf ^= 1, live = live_next) {
             const bool more = end - t0 > kWideTile;
             if (more) {
-                load(t0 + kWideTile, pg_next);
+                live_next = load(buf ^ 1, t0 + kWideTile, pg_next);
                 pg_next = page_of(end - t0 > 2 * kWideTile ? t0 + 2 * kWideTile : begin);
             }
-            if (t0 + kWideTile > w.seen && lds.bad[buf]) sort_out(buf, t0);
+            if (t0 + kWideTile > w.seen || live != ~0ull) tidy(buf, t0, live);
             if (t0 < last_lim) attend(buf, t0, live);
             if (!more) break;
-            t0 += kWideTile;
-            stage(buf ^ 1, t0);
-            live = live_next;
+            __builtin_amdgcn_s_waitcnt(0);   // the next tile's rows have arrived, then everybody's
             __syncthreads();
         }
     }
@@ -765,13 +820,13 @@ __device__ __forceinline__ void attend_wide(const PagedChunk &a, const Geo &geo,
     }
     if (n < mine) {
         const int cc = c0 + n;
-        if (w.splits == 1) {
+        if (w.parts == 1) {
             write_wide<D>(w.out + w.place<D>(a, geo, cc, 4 * h) * 2, o, any ? l : -1.f);
         } else if (h == 0) {
-            put(w.record + geo.wide * D + 2 * cc, m * scale), put(w.record + geo.wide * D + 2 * cc + 1, any ? l : -1.f);
+            put(w.record + geo.width * D + 2 * cc, m * scale), put(w.record + geo.width * D + 2 * cc + 1, any ? l : -1.f);
         }
     }
-    if (w.splits > 1) {   // as the registers hold them, so that a wave's stores lie side by side
+    if (w.parts > 1 && mine > 0) {   // as the registers hold them, so that a wave's stores lie side by side
 #pragma unroll
         for (int d = 0; d < kDims; ++d) {
 #pragma unroll
@@ -784,26 +839,21 @@ struct JoinLds {
     float sf[kJoin][16], sg[kJoin][16], sm[16], sl[16];
     unsigned arrived;
 };
-template <int D>
-union NarrowOnlyLds {
-    NarrowLds<D> narrow;
-    JoinLds join;
-};
-
-// Joins the records of `count` states of a tile, `stride` floats apart from `base` on, 16 columns
-// at a time: into the output (last), or into the first record.
+// Joins the records of the `count` shares from x0 on in steps of `step`, 16 columns at a time:
+// into the output (last), or into the first of them.
 template <int D, bool BF16>
-__device__ __forceinline__ void join_narrow(const PagedChunk &a, const Geo &geo, const Piece &w, float *base, size_t stride,
+__device__ __forceinline__ void join_narrow(const PagedChunk &a, const Geo &geo, const Piece &w, int x0, int step,
                                             int count, bool last, JoinLds &lds)
 {
+    auto record = [&](int k) { return geo.records + w.record_of(a, x0 + k * step) * geo.record; };
     for (int c0 = 0; c0 < w.cols; c0 += 16) {
         const int here = w.cols - c0 < 16 ? w.cols - c0 : 16;
-        float *states = base + geo.wide * D + 2 * c0;
+        const int states = geo.width * D + 2 * c0;
         __syncthreads();
         // each state's share of the joined one: exp2 of its maximum's distance, in sf
         for (int i = (int)threadIdx.x; i < count * here; i += kBlock) {
             const int k = i / here, ci = i - k * here;
-            const float mm = get(states + k * stride + 2 * ci), ll = get(states + k * stride + 2 * ci + 1);
+            const float mm = get(record(k) + states + 2 * ci), ll = get(record(k) + states + 2 * ci + 1);
             lds.sf[k][ci] = ll < 0.f ? -INFINITY : mm, lds.sg[k][ci] = ll;
         }
         __syncthreads();
@@ -821,39 +871,38 @@ __device__ __forceinline__ void join_narrow(const PagedChunk &a, const Geo &geo,
         __syncthreads();
         for (int i = (int)threadIdx.x; i < here * D; i += kBlock) {
             const int ci = i / D;
-            float *from = base + c0 * D + i;
             float oo = 0.f;
             for (int k0 = 0; k0 < count; k0 += 8) {   // eight on their way at a time
                 float y[8];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) y[k] = get(from + (k0 + k < count ? k0 + k : k0) * stride);
+                for (int k = 0; k < 8; ++k) y[k] = get(record(k0 + k < count ? k0 + k : k0) + c0 * D + i);
 #pragma unroll
                 for (int k = 0; k < 8; ++k)
                     if (k0 + k < count && !(lds.sg[k0 + k][ci] < 0.f)) oo += y[k] * lds.sf[k0 + k][ci];
             }
             const float ll = lds.sl[ci];
             if (last) store_out<BF16>(w.out, w.place<D>(a, geo, c0 + ci, i % D), ll < 0.f ? 0.f : oo / ll);
-            else put(from, oo);   // read by this thread alone
+            else put(record(0) + c0 * D + i, oo);   // read by this thread alone
         }
         if (!last && (int)threadIdx.x < here) {
             const int ci = (int)threadIdx.x;
-            put(states + 2 * ci, lds.sm[ci]), put(states + 2 * ci + 1, lds.sl[ci]);
+            put(record(0) + states + 2 * ci, lds.sm[ci]), put(record(0) + states + 2 * ci + 1, lds.sl[ci]);
         }
     }
 }
 
 // The same for a wide tile: a lane has the column and the elements that it had of the sum.
 template <int D>
-__device__ __forceinline__ void join_wide(const PagedChunk &a, const Geo &geo, const Piece &w, float *base, size_t stride, int count,
-                                          bool last)
+__device__ __forceinline__ void join_wide(const PagedChunk &a, const Geo &geo, const Piece &w, int x0, int step, int count, bool last)
 {
+    auto record = [&](int k) { return geo.records + w.record_of(a, x0 + k * step) * geo.record; };
     constexpr int kDims = D / 32;
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid / kWave, h = lane >> 5, cc = 32 * wave + (lane & 31);
     if (32 * wave >= w.cols) return;
-    float *states = base + geo.wide * D + 2 * (cc < w.cols ? cc : 0);
+    const int states = geo.width * D + 2 * (cc < w.cols ? cc : 0);
     float top = -INFINITY, sum = -1.f;
     for (int k = 0; k < count; ++k) {
-        const float mm = get(states + k * stride), ll = get(states + k * stride + 1);
+        const float mm = get(record(k) + states), ll = get(record(k) + states + 1);
         top = fmaxf(top, ll < 0.f ? -INFINITY : mm);
     }
     f32x16_t o[kDims];
@@ -863,16 +912,19 @@ __device__ __forceinline__ void join_wide(const PagedChunk &a, const Geo &geo, c
         for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
     }
     for (int k = 0; k < count; ++k) {
-        const float mm = get(states + k * stride), ll = get(states + k * stride + 1);
+        const float mm = get(record(k) + states), ll = get(record(k) + states + 1);
         const float f = weight(ll < 0.f ? -INFINITY : mm, top);
         if (!(ll < 0.f)) sum = (sum < 0.f ? 0.f : sum) + ll * f;
+        f32x16_t y[kDims];   // all on their way at once
 #pragma unroll
         for (int d = 0; d < kDims; ++d) {
-            float y[16];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) y[i] = get(base + k * stride + ((wave * kDims + d) * 16 + i) * kWave + lane);
+            for (int i = 0; i < 16; ++i) y[d][i] = get(record(k) + ((wave * kDims + d) * 16 + i) * kWave + lane);
+        }
 #pragma unroll
-            for (int i = 0; i < 16; ++i) o[d][i] += ll < 0.f ? 0.f : y[i] * f;
+        for (int d = 0; d < kDims; ++d) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[d][i] += ll < 0.f ? 0.f : y[d][i] * f;
         }
     }
     if (last) {
@@ -882,32 +934,31 @@ __device__ __forceinline__ void join_wide(const PagedChunk &a, const Geo &geo, c
 #pragma unroll
     for (int d = 0; d < kDims; ++d) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) put(base + ((wave * kDims + d) * 16 + i) * kWave + lane, o[d][i]);
+        for (int i = 0; i < 16; ++i) put(record(0) + ((wave * kDims + d) * 16 + i) * kWave + lane, o[d][i]);
     }
-    if (h == 0 && cc < w.cols) put(states, top), put(states + 1, sum);
+    if (h == 0 && cc < w.cols) put(record(0) + states, top), put(record(0) + states + 1, sum);
 }
 
-// The chunk's record is written; the last of the tile's chunks to arrive joins them, in the
-// order of the chunks, groups of about the square root of their number first.
+// The part's record is written; the last of the tile's parts to arrive joins them, in their
+// order, groups of about the square root of their number first.
 template <int D, bool BF16>
-__device__ __forceinline__ void join_chunks(const PagedChunk &a, const Geo &geo, const Piece &w, int slot, JoinLds &lds)
+__device__ __forceinline__ void join_parts(const PagedChunk &a, const Geo &geo, const Piece &w, JoinLds &lds)
 {
     // A record has arrived before its workgroup counts itself, and is read by the workgroup that
     // counts last; counters end at zero.
-    int group = w.splits;   // chunks of a group: at most 64, and as many groups
-    if (w.splits > 16) {
+    int group = w.parts;   // parts of a group: at most 64, and as many groups
+    if (w.parts > 16) {
         group = 16;
-        while (group * group < w.splits) group *= 2;
+        while (group * group < w.parts) group *= 2;
     }
-    static_assert((kJoin & (kJoin - 1)) == 0 && kJoin * kJoin >= kChunks + 1, "groups and their number fit the arrays");
-    const int groups = (w.splits + group - 1) / group;
+    static_assert((kJoin & (kJoin - 1)) == 0 && kJoin * kJoin >= kMostShares, "groups and their number fit the arrays");
+    const int groups = (w.parts + group - 1) / group;
     for (int level = 0; level < 2; ++level) {
-        // level 0: the chunks of this one's group, into its first record; level 1: the groups
+        // level 0: the parts of this one's group, into its first record; level 1: the groups
         if (level == 1 && groups == 1) break;
-        const int first = level == 0 ? w.split / group * group : 0;
-        const int count = level == 0 ? (w.splits - first < group ? w.splits - first : group) : groups;
-        const int step = level == 0 ? 1 : group;
-        unsigned *counter = (level == 0 ? geo.group_count : geo.tile_count) + (size_t)(slot + first) * a.Hkv + w.h;
+        const int first = level == 0 ? (w.share - w.first) / group * group : 0;
+        const int count = level == 0 ? (w.parts - first < group ? w.parts - first : group) : groups;
+        unsigned *counter = (level == 0 ? geo.group_count : geo.tile_count) + w.record_of(a, w.first + first);
         __builtin_amdgcn_s_waitcnt(0);   // this thread's stores have arrived, then everybody's
         __syncthreads();
         if (threadIdx.x == 0)
@@ -915,90 +966,133 @@ __device__ __forceinline__ void join_chunks(const PagedChunk &a, const Geo &geo,
         __syncthreads();
         if (lds.arrived != (unsigned)count - 1) return;
         if (threadIdx.x == 0 && count > 1) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        float *base = geo.records + ((size_t)(slot + first) * a.Hkv + w.h) * geo.record;
-        const size_t stride = (size_t)step * a.Hkv * geo.record;
         const bool last = level == 1 || groups == 1;
-        if constexpr (kHasWide<D, BF16>) {
-            if (w.row.width > geo.narrow) {
-                join_wide<D>(a, geo, w, base, stride, count, last);
-                continue;
-            }
-        }
-        join_narrow<D, BF16>(a, geo, w, base, stride, count, last, lds);
+        if constexpr (kHasWide<D, BF16>) join_wide<D>(a, geo, w, w.first + first, level == 0 ? 1 : group, count, last);
+        else join_narrow<D, BF16>(a, geo, w, w.first + first, level == 0 ? 1 : group, count, last, lds);
     }
 }
 
 template <int D, bool BF16>
 union Lds {
-    NarrowLds<D> narrow;
-    WideLds<D> wide;
+    std::conditional_t<kHasWide<D, BF16>, WideLds<D>, NarrowLds<D>> attend;
     JoinLds join;
 };
 
+// Waves a SIMD, and workgroups a CU: as many as the registers hold.
+constexpr int occupancy(int D, bool bf16) { return D <= (bf16 ? 64 : 32) ? 3 : 2; }
+
 template <int D, bool BF16>
-__global__ __launch_bounds__(kBlock, 2) void paged_chunk_kernel(PagedChunk a, Geo geo)
+__global__ __launch_bounds__(kBlock, (occupancy(D, BF16))) void paged_chunk_kernel(PagedChunk a, Geo geo)
 {
-    using Shared = std::conditional_t<kHasWide<D, BF16>, Lds<D, BF16>, NarrowOnlyLds<D>>;
-    __shared__ __align__(16) Shared lds;
+    __shared__ __align__(16) Lds<D, BF16> lds;
+    __shared__ Rows rows;
 
     const unsigned wg = wide_index();
-    const int t = (int)geo.by_hkv(wg);
     Piece p;
-    p.h = (int)wg - t * a.Hkv;
-    Task task;
-    if (geo.plan ? !find_planned(geo.plan, a.R, t, task) : !find_task(a, geo, t, task)) return;
-
-    p.r = task.r;
-    p.row = row_of(a, geo, a.kv_len[task.r], a.offsets[task.r], a.offsets[task.r + 1]);
-    // offsets that decrease would lead past the output and the records
-    if ((unsigned)task.tile >= (unsigned)p.row.tiles || (unsigned)task.split >= (unsigned)task.splits ||
-        (task.splits > 1 && (task.slot < 0 || ((long long)task.slot + task.splits) * a.Hkv > geo.slots)))
-        return;
-    p.col0 = task.tile * p.row.width;
-    p.cols = p.row.columns - p.col0 < p.row.width ? p.row.columns - p.col0 : p.row.width;
-    const int L = p.limit(a, geo, p.col0 + p.cols - 1);
-    p.seen = p.limit(a, geo, p.col0);
-    const int units = units_of(L), per = (units + task.splits - 1) / task.splits;
-    p.splits = (units + per - 1) / per;   // an early tile may have fewer chunks than the row's last
-    p.split = task.split;
-    if (p.split >= p.splits) return;
-    p.begin = p.split * per * kUnit;
-    p.end = L - p.begin < per * (long long)kUnit ? L : p.begin + per * kUnit;
-    p.out = a.out + ((size_t)p.row.begin * a.Hq + (size_t)p.h * geo.G) * D * (BF16 ? 2 : 4);
-    p.record = geo.records + ((size_t)(task.slot + p.split) * a.Hkv + p.h) * geo.record;
-    if constexpr (kHasWide<D, BF16>) {
-        if (p.row.width > geo.narrow) attend_wide<D>(a, geo, p, lds.wide);
-        else attend_narrow<D, BF16>(a, geo, p, lds.narrow);
-    } else {
-        attend_narrow<D, BF16>(a, geo, p, lds.narrow);
+    p.share = (int)geo.by_hkv(wg);
+    if (p.share >= geo.shares) return;
+    p.h = (int)wg - p.share * a.Hkv;
+    if (!geo.plan) {
+        if (threadIdx.x < kWave) add_rows(a, geo, rows);
+        __syncthreads();
     }
-    if (p.splits > 1) join_chunks<D, BF16>(a, geo, p, task.slot, lds.join);
+    const u64_t *sums = geo.plan ? geo.plan : rows.sums;
+    const u64_t all = uniform64(sums[a.R]);
+    u64_t share = (all + (unsigned)geo.shares - 1) / (unsigned)geo.shares;
+    // Whole tiles take the longest's time or the mean of the shares.  Cut ones take that, a part's
+    // record and the joining, and find less of their keys in the L2 (us, whole and cut: 2048
+    // tokens over 32500 positions 1436 and 1618, 32 prompts of 1 to 1164 tokens 75 and 87;
+    // 32 rows of 5 tokens over 200 to 4096 167 and 74, 512 tokens over 8192 262 and 121).
+    bool whole = false;
+    if (!geo.plan) {
+        const float mean = (float)share, longest = (float)(rows.longest * kUnit + kStart);
+        const float cut = 1.12f * fmaxf(mean, (float)kLeast) + 3 * kStart;
+        whole = (rows.tiles <= geo.shares ? longest : 1.05f * fmaxf(longest, mean)) <= cut;
+    }
+    share = share < kLeast ? kLeast : share;
+
+    auto attend = [&]() {
+        p.col0 = p.tile * geo.width;
+        p.cols = p.row.columns - p.col0 < geo.width ? p.row.columns - p.col0 : geo.width;
+        p.seen = p.limit(a, geo, p.col0);
+        p.out = a.out + ((size_t)p.row.begin * a.Hq + (size_t)p.h * geo.G) * D * (BF16 ? 2 : 4);
+        p.record = geo.records + p.record_of(a, p.share) * geo.record;
+        if constexpr (kHasWide<D, BF16>) attend_wide<D>(a, geo, p, lds.attend);
+        else attend_narrow<D, BF16>(a, geo, p, lds.attend);
+    };
+    auto last_limit = [&]() {   // of the tile's last column
+        const int behind = (p.tile + 1) * geo.width;
+        return p.limit(a, geo, (behind < p.row.columns ? behind : p.row.columns) - 1);
+    };
+
+    if (whole) {
+        const int tiles = __builtin_amdgcn_readfirstlane(rows.tiles);
+        p.first = p.share, p.parts = 1;
+        for (int turn = 0, t = p.share; t < tiles; ++turn) {
+            if (threadIdx.x < kWave) find_tile(a, geo, rows, t);
+            __syncthreads();
+            p.r = __builtin_amdgcn_readfirstlane(rows.row), p.tile = __builtin_amdgcn_readfirstlane(rows.tile);
+            p.row = row_of(a, geo, rows.len[p.r], rows.off[p.r], rows.off[p.r + 1]);
+            p.begin = 0, p.end = last_limit();
+            attend();
+            // there and back again: who had the longest of a turn has the shortest of the next
+            t = (turn + 1) * geo.shares + (turn & 1 ? p.share : geo.shares - 1 - p.share);
+            __syncthreads();   // everybody has left the tile in LDS
+        }
+        return;
+    }
+    const u64_t begin = share * (unsigned)p.share, end = begin + share < all ? begin + share : all;
+    for (u64_t x = begin; x < end;) {
+        p.r = row_at(sums, a.R, x);
+        const u64_t row_begin = uniform64(sums[p.r]);
+        p.row = row_of(a, geo, a.kv_len[p.r], a.offsets[p.r], a.offsets[p.r + 1]);
+        p.tile = __builtin_amdgcn_readfirstlane(tile_at(a, geo, p.row, x - row_begin));
+        const u64_t t0 = row_begin + uniform64(work_before(a, geo, p.row, p.tile));
+        const u64_t t1 = row_begin + uniform64(work_before(a, geo, p.row, p.tile + 1));
+        x = t1;
+        // The tile's units before the border of two shares, as both and the tile's others reckon
+        // them.  A border within half a unit of the tile's begins or ends there.
+        const int L = last_limit(), units = units_of(L);
+        auto unit_at = [&](u64_t at) {
+            const int u = at <= t0 ? 0 : at >= t1 ? units : (int)((double)units * ((double)(at - t0) / (double)(t1 - t0)) + 0.5);
+            return __builtin_amdgcn_readfirstlane(u < units ? u : units);
+        };
+        p.first = (int)(t0 / share);
+        int last = (int)((t1 - 1) / share);
+        if (last > p.first && unit_at(share * (unsigned)(p.first + 1)) == 0) ++p.first;
+        if (last > p.first && unit_at(share * (unsigned)last) == units) --last;
+        if (p.share < p.first || p.share > last) continue;
+        p.parts = last - p.first + 1;
+        p.begin = p.share == p.first ? 0 : unit_at(begin) * kUnit;   // below 2^31: a unit of the row's
+        const long long stop = p.share == last ? L : (long long)unit_at(begin + share) * kUnit;
+        p.end = stop < L ? (int)stop : L;
+        attend();
+        if (p.parts > 1) join_parts<D, BF16>(a, geo, p, lds.join);
+        __syncthreads();   // everybody has left the tile in LDS
+    }
 }
 
 struct Layout {
-    int narrow, wide, record;
-    long long grid, slots;   // workgroups and records at most
+    int width, record, shares;
     size_t tile_count, plan, records, bytes;   // byte offsets in the workspace
 };
 
 Layout layout_of(int N, int R, int Hq, int Hkv, int page, int cols, int D, bool bf16) {
     Layout y{};
-    const long long columns = (long long)N * (Hq / Hkv);
-    y.narrow = bf16 || D <= 64 ? 32 : 16;
-    y.wide = bf16 && D >= 32 && columns > y.narrow ? kWideColumns : y.narrow;
-    y.record = y.wide * (D + 2);
-    const long long rows = R < N ? R : N;   // with tokens
-    const long long tiles = (columns / y.wide + rows) * Hkv;
-    const long long most = ((long long)cols * page + kUnit - 1) / kUnit, units = most < 1 ? 1 : most;
-    // c units a chunk, work / kChunks at least: chunks are kChunks and one begun per tile at most,
-    // and a cut tile's are more than half used on average
-    y.grid = kChunks + tiles < tiles * units ? kChunks + tiles : tiles * units;
-    y.slots = 2ll * kChunks < tiles * units ? 2ll * kChunks : tiles * units;
+    y.width = bf16 ? (D >= 32 ? kWideColumns : 32) : D <= 64 ? 32 : 16;
+    y.record = y.width * (D + 2);
+    const int places = 256 * occupancy(D, bf16);   // workgroups that fit the 256 CUs at once
+    // all places to the heads alike; two rounds of them where that would leave many empty
+    long long shares = Hkv <= places / 8 ? places / Hkv : 2 * places / Hkv;
+    const long long columns = (long long)N * (Hq / Hkv), rows = R < N ? R : N;   // rows with tokens
+    const long long tiles = columns / y.width + rows, units = ((long long)cols * page + kUnit - 1) / kUnit + 1;
+    if (shares > tiles * units) shares = tiles * units;
+    y.shares = shares < 1 ? 1 : (int)shares;
     // the counters lie where every call has them, whatever its sizes
-    y.tile_count = 2 * kChunks * sizeof(unsigned);
+    y.tile_count = 2 * kMostShares * sizeof(unsigned);
     y.plan = 2 * y.tile_count;
-    y.records = y.plan + (R > kScanRows ? ((size_t)R + 1) * sizeof(int4) : 0);
-    y.bytes = y.records + (units > 1 ? (size_t)y.slots * y.record * sizeof(float) : 0);
+    y.records = y.plan + (R > kScanRows ? ((size_t)R + 2) / 2 * 2 * sizeof(u64_t) : 0);
+    y.bytes = y.records + (y.shares > 1 ? 2 * (size_t)y.shares * Hkv * y.record * sizeof(float) : 0);
     return y;
 }
 
@@ -1012,20 +1106,20 @@ hipError_t launch_paged_chunk_attn(const PagedChunk &a, int D, bool bf16, hipStr
 {
     const Layout y = layout_of(a.N, a.R, a.Hq, a.Hkv, a.cache.page, a.cache.cols, D, bf16);
     Geo geo{};
-    geo.G = a.Hq / a.Hkv, geo.narrow = y.narrow, geo.wide = y.wide, geo.record = y.record, geo.slots = y.slots;
+    geo.G = a.Hq / a.Hkv, geo.width = y.width, geo.half = 0.5 * y.width / geo.G, geo.record = y.record, geo.shares = y.shares;
     geo.by_page = make_div(a.cache.page), geo.by_hkv = make_div(a.Hkv), geo.by_g = make_div(geo.G);
     geo.page16 = (unsigned)(a.cache.page_bytes / 16), geo.slot16 = (unsigned)(a.cache.slot_bytes / 16);
     geo.group_count = reinterpret_cast<unsigned *>(a.workspace);
     geo.tile_count = reinterpret_cast<unsigned *>(a.workspace + y.tile_count);
     geo.records = reinterpret_cast<float *>(a.workspace + y.records);
     if (a.R > kScanRows) {
-        auto *plan = reinterpret_cast<int4 *>(a.workspace + y.plan);
+        auto *plan = reinterpret_cast<u64_t *>(a.workspace + y.plan);
         geo.plan = plan;
         hipLaunchKernelGGL(chunk_plan_kernel, dim3(1), dim3(1024), 0, stream, a, geo, plan);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    const dim3 gd = wide_grid(y.grid), bd(kBlock);
+    const dim3 gd = wide_grid((long long)y.shares * a.Hkv), bd(kBlock);
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, gd, bd, 0, stream, a, geo); };
     switch (D) {
     case 16: bf16 ? launch(paged_chunk_kernel<16, true>) : launch(paged_chunk_kernel<16, false>); break;
