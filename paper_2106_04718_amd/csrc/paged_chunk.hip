@@ -757,7 +757,6 @@ __device__ __forceinline__ void attend_wide(const PagedChunk &a, const Geo &geo,
     // elements are added to the columns that do and taken out.
     auto tidy = [&](int buf, int t0, unsigned long long live) {
         constexpr int kMine = kWideTile * D * 2 / 16 / kBlock;   // 16-byte pieces of a lane's
-        if (tid == 0) lds.bad = 0u;
         bool bad = false;
 #pragma unroll
         for (int i = 0; i < kMine; ++i) {
@@ -770,10 +769,9 @@ __device__ __forceinline__ void attend_wide(const PagedChunk &a, const Geo &geo,
                 for (int j = 0; j < 4; ++j) bad |= ((*x)[j] & 0x7f80u) == 0x7f80u || ((*x)[j] & 0x7f800000u) == 0x7f800000u;
             }
         }
-        __syncthreads();
         if (__any(bad) && lane == 0) lds.bad = 1u;
         __syncthreads();
-        if (!lds.bad) return;
+        if (!lds.bad) return;   // 0 from the beginning
         for (int key = 0; key < kWideTile; ++key) {
 #pragma unroll
             for (int d = 0; d < kDims; ++d) {
@@ -790,6 +788,7 @@ __device__ __forceinline__ void attend_wide(const PagedChunk &a, const Geo &geo,
             auto *x = reinterpret_cast<uint16_t *>(lds.v[buf] + Lds::value(i / D)) + i % D;
             if ((*x & 0x7f80u) == 0x7f80u) *x = 0;
         }
+        if (tid == 0) lds.bad = 0u;
         __syncthreads();
     };
 
@@ -797,6 +796,7 @@ __device__ __forceinline__ void attend_wide(const PagedChunk &a, const Geo &geo,
         int pg = page_of(begin), buf = 0;
         int pg_next = page_of(end - begin > kWideTile ? begin + kWideTile : begin);
         unsigned long long live = load(0, begin, pg), live_next = 0;
+        if (tid == 0) lds.bad = 0u;
         __builtin_amdgcn_s_waitcnt(0);
         __syncthreads();
         for (int t0 = begin;; t0 += kWideTile, buf ^= 1, live = live_next) {
@@ -1000,75 +1000,74 @@ __global__ __launch_bounds__(kBlock, (occupancy(D, BF16))) void paged_chunk_kern
     const u64_t all = uniform64(sums[a.R]);
     u64_t share = (all + (unsigned)geo.shares - 1) / (unsigned)geo.shares;
     // Whole tiles take the longest's time or the mean of the shares.  Cut ones take that, a part's
-    // record and the joining, and find less of their keys in the L2 (us, whole and cut: 2048
+    // record and the joining, and wide ones find less of their keys in the L2 (us, whole and cut: 2048
     // tokens over 32500 positions 1436 and 1618, 32 prompts of 1 to 1164 tokens 75 and 87;
     // 32 rows of 5 tokens over 200 to 4096 167 and 74, 512 tokens over 8192 262 and 121).
     bool whole = false;
     if (!geo.plan) {
         const float mean = (float)share, longest = (float)(rows.longest * kUnit + kStart);
-        const float cut = 1.12f * fmaxf(mean, (float)kLeast) + 3 * kStart;
+        const float least = fmaxf(mean, (float)kLeast), cut = 1.12f * least + 3 * kStart;
         whole = (rows.tiles <= geo.shares ? longest : 1.05f * fmaxf(longest, mean)) <= cut;
     }
     share = share < kLeast ? kLeast : share;
 
-    auto attend = [&]() {
+    const u64_t begin = share * (unsigned)p.share, end = begin + share < all ? begin + share : all;
+    const int tiles = geo.plan ? 0 : __builtin_amdgcn_readfirstlane(rows.tiles);
+    u64_t x = begin;                  // of its share, done so far
+    int turn = 0, t = p.share;        // or its next tile
+    auto known = [&](int r) {
+        auto same = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+        return row_of(a, geo, same(rows.len[r]), same(rows.off[r]), same(rows.off[r + 1]));
+    };
+    for (;; __syncthreads()) {   // everybody has left the tile in LDS
+        if (whole) {
+            if (t >= tiles) return;
+            if (threadIdx.x < kWave) find_tile(a, geo, rows, t);
+            // there and back again: who had the longest of a turn has the shortest of the next
+            ++turn;
+            t = turn * geo.shares + (turn & 1 ? geo.shares - 1 - p.share : p.share);
+            __syncthreads();
+            p.r = __builtin_amdgcn_readfirstlane(rows.row), p.tile = __builtin_amdgcn_readfirstlane(rows.tile);
+            p.row = known(p.r);
+        } else {
+            if (x >= end) return;
+            p.r = row_at(sums, a.R, x);
+            p.row = geo.plan ? row_of(a, geo, a.kv_len[p.r], a.offsets[p.r], a.offsets[p.r + 1]) : known(p.r);
+            p.tile = __builtin_amdgcn_readfirstlane(tile_at(a, geo, p.row, x - uniform64(sums[p.r])));
+        }
         p.col0 = p.tile * geo.width;
         p.cols = p.row.columns - p.col0 < geo.width ? p.row.columns - p.col0 : geo.width;
         p.seen = p.limit(a, geo, p.col0);
+        const int L = p.limit(a, geo, p.col0 + p.cols - 1);
         p.out = a.out + ((size_t)p.row.begin * a.Hq + (size_t)p.h * geo.G) * D * (BF16 ? 2 : 4);
+        p.first = p.share, p.parts = 1;
+        p.begin = 0, p.end = L;
+        if (!whole) {
+            const u64_t row_begin = uniform64(sums[p.r]);
+            const u64_t t0 = row_begin + uniform64(work_before(a, geo, p.row, p.tile));
+            const u64_t t1 = row_begin + uniform64(work_before(a, geo, p.row, p.tile + 1));
+            x = t1;
+            // The tile's units before the border of two shares, as both and the tile's others
+            // reckon them.  A border within half a unit of the tile's begins or ends there.
+            const int units = units_of(L);
+            auto unit_at = [&](u64_t at) {
+                const int u = at <= t0 ? 0 : at >= t1 ? units : (int)((double)units * ((double)(at - t0) / (double)(t1 - t0)) + 0.5);
+                return __builtin_amdgcn_readfirstlane(u < units ? u : units);
+            };
+            p.first = (int)(t0 / share);
+            int last = (int)((t1 - 1) / share);
+            if (last > p.first && unit_at(share * (unsigned)(p.first + 1)) == 0) ++p.first;
+            if (last > p.first && unit_at(share * (unsigned)last) == units) --last;
+            if (p.share < p.first || p.share > last) continue;
+            p.parts = last - p.first + 1;
+            if (p.share > p.first) p.begin = unit_at(begin) * kUnit;   // below 2^31: a unit of the row's
+            const long long stop = p.share == last ? L : (long long)unit_at(begin + share) * kUnit;
+            p.end = stop < L ? (int)stop : L;
+        }
         p.record = geo.records + p.record_of(a, p.share) * geo.record;
         if constexpr (kHasWide<D, BF16>) attend_wide<D>(a, geo, p, lds.attend);
         else attend_narrow<D, BF16>(a, geo, p, lds.attend);
-    };
-    auto last_limit = [&]() {   // of the tile's last column
-        const int behind = (p.tile + 1) * geo.width;
-        return p.limit(a, geo, (behind < p.row.columns ? behind : p.row.columns) - 1);
-    };
-
-    if (whole) {
-        const int tiles = __builtin_amdgcn_readfirstlane(rows.tiles);
-        p.first = p.share, p.parts = 1;
-        for (int turn = 0, t = p.share; t < tiles; ++turn) {
-            if (threadIdx.x < kWave) find_tile(a, geo, rows, t);
-            __syncthreads();
-            p.r = __builtin_amdgcn_readfirstlane(rows.row), p.tile = __builtin_amdgcn_readfirstlane(rows.tile);
-            p.row = row_of(a, geo, rows.len[p.r], rows.off[p.r], rows.off[p.r + 1]);
-            p.begin = 0, p.end = last_limit();
-            attend();
-            // there and back again: who had the longest of a turn has the shortest of the next
-            t = (turn + 1) * geo.shares + (turn & 1 ? p.share : geo.shares - 1 - p.share);
-            __syncthreads();   // everybody has left the tile in LDS
-        }
-        return;
-    }
-    const u64_t begin = share * (unsigned)p.share, end = begin + share < all ? begin + share : all;
-    for (u64_t x = begin; x < end;) {
-        p.r = row_at(sums, a.R, x);
-        const u64_t row_begin = uniform64(sums[p.r]);
-        p.row = row_of(a, geo, a.kv_len[p.r], a.offsets[p.r], a.offsets[p.r + 1]);
-        p.tile = __builtin_amdgcn_readfirstlane(tile_at(a, geo, p.row, x - row_begin));
-        const u64_t t0 = row_begin + uniform64(work_before(a, geo, p.row, p.tile));
-        const u64_t t1 = row_begin + uniform64(work_before(a, geo, p.row, p.tile + 1));
-        x = t1;
-        // The tile's units before the border of two shares, as both and the tile's others reckon
-        // them.  A border within half a unit of the tile's begins or ends there.
-        const int L = last_limit(), units = units_of(L);
-        auto unit_at = [&](u64_t at) {
-            const int u = at <= t0 ? 0 : at >= t1 ? units : (int)((double)units * ((double)(at - t0) / (double)(t1 - t0)) + 0.5);
-            return __builtin_amdgcn_readfirstlane(u < units ? u : units);
-        };
-        p.first = (int)(t0 / share);
-        int last = (int)((t1 - 1) / share);
-        if (last > p.first && unit_at(share * (unsigned)(p.first + 1)) == 0) ++p.first;
-        if (last > p.first && unit_at(share * (unsigned)last) == units) --last;
-        if (p.share < p.first || p.share > last) continue;
-        p.parts = last - p.first + 1;
-        p.begin = p.share == p.first ? 0 : unit_at(begin) * kUnit;   // below 2^31: a unit of the row's
-        const long long stop = p.share == last ? L : (long long)unit_at(begin + share) * kUnit;
-        p.end = stop < L ? (int)stop : L;
-        attend();
         if (p.parts > 1) join_parts<D, BF16>(a, geo, p, lds.join);
-        __syncthreads();   // everybody has left the tile in LDS
     }
 }
 
