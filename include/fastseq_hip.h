@@ -753,8 +753,9 @@ size_t fs_paged_chunk_attn_workspace_bytes(int N, int R, int Hq, int Hkv, int pa
  *                replayed from graphs.
  *   stream       hipStream_t (NULL = default stream)
  * Supported: fs_paged_append's set; Hq a multiple of Hkv, N * Hq <= 2^28, R <= 2^24.
- * Arithmetic: products and sums in fp32, one rounding at the end.  The bits depend on
- * the data and the sizes, never on run or launch.
+ * Arithmetic: products and sums in fp32, one rounding at the end; for a bf16 cache
+ * each weight is the sum of two bf16 values, within 2^-17 of it.  The bits depend on the
+ * data and the sizes, never on run or launch.
  * Errors: those of fs_paged_attn for the arguments that both have.  N, R or Hq == 0
  * returns FS_OK with no launch.
  */
