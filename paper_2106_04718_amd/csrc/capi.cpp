@@ -1049,6 +1049,8 @@ int fs_rotary(const void *q, int64_t q_token_stride, int64_t q_head_stride, cons
                     (const void *)positions, (const void *)freq);
     if (!aligned(positions, 4) || !aligned(freq, 8)) return fail(FS_ERR_INVALID_ARG, "positions and freq must be aligned to their elements");
     const long long e = dtype == FS_BF16 ? 2 : 4;
+    if ((long long)N * (Hq + Hkv) * (D * e / 16) > (long long)INT_MAX * 128)
+        return fail(FS_ERR_UNSUPPORTED, "too many tokens for one launch (N=%d Hq=%d Hkv=%d D=%d)", N, Hq, Hkv, D);
     const int64_t per16 = 16 / e;
     struct {
         const void *p;

@@ -112,7 +112,8 @@ __device__ __forceinline__ u64_t uniform64(u64_t x) {
 struct Rows {
     u64_t sums[kScanRows + 1];   // work before each of them, and of all
     int len[kScanRows], off[kScanRows + 1];
-    int longest, tiles;          // units of the longest tile, and tiles of a head
+    int tiles[kScanRows + 1];    // of a head before each of them, and of all
+    int longest;                 // units of the longest
     int row, tile;               // where tiles are taken whole: the one found
 };
 
@@ -134,23 +135,24 @@ __device__ __forceinline__ void add_rows(const PagedChunk &a, const Geo &geo, Ro
 #pragma unroll
     for (int i = 0; i < 5; ++i) off[i] = a.offsets[4 * lane + i < a.R ? 4 * lane + i : a.R];
     u64_t work[4], sum = 0;
-    int longest = 0, tiles = 0;
+    int longest = 0, tiles[4], all_tiles = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const Row w = row_of(a, geo, len[i], off[i], off[i + 1]);   // none behind the last row: it would begin at its end
         work[i] = work_before(a, geo, w, w.tiles), sum += work[i];
         const int u = w.tiles ? units_of(len[i] < cap ? len[i] : cap) : 0;
-        longest = longest > u ? longest : u, tiles += w.tiles;
+        longest = longest > u ? longest : u, tiles[i] = w.tiles, all_tiles += w.tiles;
         rows.len[4 * lane + i] = len[i], rows.off[4 * lane + i] = off[i];
     }
     u64_t at = wave_scan64(sum) - sum;
+    int tile = wave_scan(all_tiles) - all_tiles;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        rows.sums[4 * lane + i] = at;
-        at += work[i];
+        rows.sums[4 * lane + i] = at, rows.tiles[4 * lane + i] = tile;
+        at += work[i], tile += tiles[i];
     }
-    longest = wave_max(longest), tiles = wave_sum(tiles);
-    if (lane == 63) rows.sums[kScanRows] = at, rows.off[kScanRows] = off[4], rows.longest = longest, rows.tiles = tiles;
+    longest = wave_max(longest);
+    if (lane == 63) rows.sums[kScanRows] = at, rows.off[kScanRows] = off[4], rows.tiles[kScanRows] = tile, rows.longest = longest;
 }
 
 // The first tile of a row with at least x units (its tiles if there is none).
@@ -219,14 +221,15 @@ __global__ __launch_bounds__(1024) void chunk_plan_kernel(PagedChunk a, Geo geo,
     if (tid == 0) sums[a.R] = before;
 }
 
-// The last row whose work begins at or before x, 64 looked at at a time.
-__device__ __forceinline__ int row_at(const u64_t *sums, int R, u64_t x) {
+// The last row whose work (or tiles) begins at or before x, 64 looked at at a time.
+template <typename T>
+__device__ __forceinline__ int row_at(const T *sums, int R, T x) {
     const int lane = (int)threadIdx.x & 63;
     int lo = 0, n = R;
     while (n > 1) {
         const int step = (n + 63) / 64, at = lane * step;
         const bool there = at < n && lo + at < R;
-        const u64_t v = sums[there ? lo + at : 0];
+        const T v = sums[there ? lo + at : 0];
         lo += step * (63 - __clzll((long long)__ballot(lane == 0 || (there && v <= x))));
         n = step;
     }
@@ -1007,12 +1010,12 @@ __global__ __launch_bounds__(kBlock, (occupancy(D, BF16))) void paged_chunk_kern
     if (!geo.plan) {
         const float mean = (float)share, longest = (float)(rows.longest * kUnit + kStart);
         const float least = fmaxf(mean, (float)kLeast), cut = 1.12f * least + 3 * kStart;
-        whole = (rows.tiles <= geo.shares ? longest : 1.05f * fmaxf(longest, mean)) <= cut;
+        whole = (rows.tiles[kScanRows] <= geo.shares ? longest : 1.05f * fmaxf(longest, mean)) <= cut;
     }
     share = share < kLeast ? kLeast : share;
 
     const u64_t begin = share * (unsigned)p.share, end = begin + share < all ? begin + share : all;
-    const int tiles = geo.plan ? 0 : __builtin_amdgcn_readfirstlane(rows.tiles);
+    const int tiles = geo.plan ? 0 : __builtin_amdgcn_readfirstlane(rows.tiles[kScanRows]);
     u64_t x = begin;                  // of its share, done so far
     int turn = 0, t = p.share;        // or its next tile
     auto known = [&](int r) {
@@ -1022,12 +1025,18 @@ __global__ __launch_bounds__(kBlock, (occupancy(D, BF16))) void paged_chunk_kern
     for (;; __syncthreads()) {   // everybody has left the tile in LDS
         if (whole) {
             if (t >= tiles) return;
-            if (threadIdx.x < kWave) find_tile(a, geo, rows, t);
-            // there and back again: who had the longest of a turn has the shortest of the next
-            ++turn;
-            t = turn * geo.shares + (turn & 1 ? geo.shares - 1 - p.share : p.share);
-            __syncthreads();
-            p.r = __builtin_amdgcn_readfirstlane(rows.row), p.tile = __builtin_amdgcn_readfirstlane(rows.tile);
+            if (tiles <= geo.shares) {   // one each: in any order
+                p.r = row_at(rows.tiles, a.R, t);
+                p.tile = t - __builtin_amdgcn_readfirstlane(rows.tiles[p.r]);
+                t = tiles;
+            } else {
+                if (threadIdx.x < kWave) find_tile(a, geo, rows, t);
+                // there and back again: who had the longest of a turn has the shortest of the next
+                ++turn;
+                t = turn * geo.shares + (turn & 1 ? geo.shares - 1 - p.share : p.share);
+                __syncthreads();
+                p.r = __builtin_amdgcn_readfirstlane(rows.row), p.tile = __builtin_amdgcn_readfirstlane(rows.tile);
+            }
             p.row = known(p.r);
         } else {
             if (x >= end) return;

@@ -22,6 +22,7 @@ namespace fs {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kMany = 2;   // units of a lane on their way together
 
 // Cosine and sine of p * f, f in radians.  What is left of the angle behind the nearest
 // quarter turn is at most pi / 4; the series end where a term is below 2^-28.
@@ -43,13 +44,10 @@ __device__ __forceinline__ float2 turn(int p, double f) {
     return make_float2(quadrant == 1 || quadrant == 2 ? -a : a, quadrant >= 2 ? -b : b);
 }
 
-// VEC elements of a row.
-template <bool BF16, int VEC>
+// 16 bytes of a row.
+template <bool BF16>
 struct Piece {
-    static constexpr int kBytes = VEC * (BF16 ? 2 : 4);
-    using Word = std::conditional_t<kBytes == 2, uint16_t, uint32_t>;
-    static constexpr int kWords = kBytes < 4 ? 1 : kBytes / 4;
-    typedef Word words_t __attribute__((ext_vector_type(kWords)));
+    typedef uint32_t words_t __attribute__((ext_vector_type(4)));
     words_t w;
 
     __device__ __forceinline__ void load(const unsigned char *p) {
@@ -58,7 +56,6 @@ struct Piece {
     __device__ __forceinline__ void store(unsigned char *p) const { *reinterpret_cast<words_t *>(p) = w; }
     __device__ __forceinline__ float get(int e) const {
         if constexpr (!BF16) return __uint_as_float(w[e]);
-        else if constexpr (VEC == 1) return __uint_as_float((uint32_t)w[0] << 16);
         else return __uint_as_float(e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
     }
     __device__ __forceinline__ void set(int e, float x) {
@@ -66,77 +63,104 @@ struct Piece {
             w[e] = __float_as_uint(x);
         } else {
             const uint32_t b = __builtin_bit_cast(uint16_t, (__bf16)x);
-            if constexpr (VEC == 1) w[0] = (uint16_t)b;
-            else w[e / 2] = e & 1 ? (w[e / 2] & 0xffffu) | b << 16 : (w[e / 2] & 0xffff0000u) | b;
+            w[e / 2] = e & 1 ? (w[e / 2] & 0xffffu) | b << 16 : (w[e / 2] & 0xffff0000u) | b;
         }
     }
 };
 
-// A unit is VEC pairs of a head, two pieces: units below `turned` hold pairs to be turned
-// (interleaved: the last of them perhaps elements behind rot too), the others elements that
-// are copied.  A workgroup has the units of `tokens` tokens, kAhead of a lane's on their way
-// together.
-constexpr int kAhead = 4;
-template <bool BF16, int VEC, bool INTER>
-__global__ __launch_bounds__(kThreads) void rotary_kernel(Rotary a, int tokens, int turned, Div by_units, int units, Div by_heads,
-                                                          Div by_pairs)
+// How a lane's elements meet their partners:
+//   kInter   a unit is 32 bytes of a head, pairs side by side
+//   kHalves  16 bytes of the first half of rot and 16 of the second
+//   kAnyHalf 16 bytes of a head, whose partners lie anywhere in rot: they come from LDS
+// Units below `turned` hold elements to be turned (kInter, kAnyHalf: the last of them perhaps
+// elements behind rot too); the others are copied.  Units are numbered along all tokens and heads,
+// and a workgroup has `batch` of them, AHEAD a lane, whose loads are on their way together: with
+// whole tokens a workgroup instead, some lanes would go round more often than others (9000
+// tokens of 72 heads of 128, 332 MB, 73 us; 16384 of 40 64).  In place nothing behind `turned`
+// is stored.
+enum class Pairs { kInter, kHalves, kAnyHalf };
+template <bool BF16, Pairs PAIRS, int AHEAD>
+__global__ __launch_bounds__(kThreads) void rotary_kernel(Rotary a, int batch, int turned, int stored, Div by_token, int token_units,
+                                                          Div by_units, int units, Div by_pairs)
 {
-    extern __shared__ float2 turns[];   // [tokens][pairs]
-    using P = Piece<BF16, VEC>;
-    constexpr int kEsize = BF16 ? 2 : 4;
-    const int pairs = a.rot / 2, heads = a.Hq + a.Hkv;
-    const long long n0 = (long long)wide_index() * tokens;
-    if (n0 >= a.N) return;
-    const int here = a.N - n0 < tokens ? (int)(a.N - n0) : tokens;
-    const int all = here * heads * units;
+    extern __shared__ __align__(16) unsigned char lds[];
+    constexpr int kVec = BF16 ? 8 : 4, kEsize = BF16 ? 2 : 4;
+    constexpr bool kInter = PAIRS == Pairs::kInter, kTwo = PAIRS != Pairs::kAnyHalf;
+    using P = Piece<BF16>;
+    const int pairs = a.rot / 2;
+    const unsigned long long begin = (unsigned long long)wide_index() * (unsigned)batch, end = (unsigned long long)a.N * (unsigned)token_units;
+    if (begin >= end) return;
+    const int all = end - begin < (unsigned)batch ? (int)(end - begin) : batch;
+    const int n0 = begin < 0x7fffffffu ? (int)by_token((unsigned)begin) : (int)(begin / (unsigned)token_units);
+    const int behind = (int)(begin - (unsigned long long)(unsigned)n0 * (unsigned)token_units);   // units of token n0 before the first
+    const int tokens = (int)by_token((unsigned)(behind + all - 1)) + 1;
+    float2 *turns = reinterpret_cast<float2 *>(lds + (kTwo ? 0 : AHEAD * kThreads * 16));   // [tokens][pairs], behind what the lanes hold
 
-    for (int i0 = 0, first = 1; i0 < all; i0 += kAhead * kThreads, first = 0) {
-        P x[kAhead], y[kAhead];
-        unsigned char *to[kAhead], *to2[kAhead];
-        int at[kAhead], unit[kAhead];
+    P x[AHEAD], y[AHEAD];
+    unsigned char *to[AHEAD], *to2[AHEAD];
+    int at[AHEAD], unit[AHEAD];
 #pragma unroll
-        for (int e = 0; e < kAhead; ++e) {
-            const int mine = i0 + e * kThreads + (int)threadIdx.x, i = mine < all ? mine : all - 1;   // past the last: not stored
-            const int th = (int)by_units((unsigned)i), t = (int)by_heads((unsigned)th), h = th - t * heads;
-            unit[e] = i - th * units;
-            const bool half = !INTER && unit[e] < turned;
-            const int d = half ? unit[e] * VEC : 2 * unit[e] * VEC;   // behind rot both layouts go on in twos
-            const size_t next = (size_t)(half ? pairs : VEC) * kEsize;
-            const bool key = h >= a.Hq;
-            const RotaryRows &r = key ? a.k : a.q;
-            const long long n = n0 + t, hh = key ? h - a.Hq : h;
-            const unsigned char *from = r.from + n * r.from_token + hh * r.from_head + (size_t)d * kEsize;
-            to[e] = r.to + n * r.to_token + hh * r.to_head + (size_t)d * kEsize, to2[e] = to[e] + next;
-            at[e] = mine < all ? t * pairs : -1;
-            x[e].load(from), y[e].load(from + next);
-        }
-        if (first) {
-            for (int i = (int)threadIdx.x; i < here * pairs; i += kThreads) {
-                const int t = (int)by_pairs((unsigned)i), p = i - t * pairs;
-                const float2 cs = turn(a.positions[n0 + t], a.freq[p]);
-                turns[i] = make_float2(cs.x * a.magnitude, cs.y * a.magnitude);
-            }
-            __syncthreads();
-        }
+    for (int e = 0; e < AHEAD; ++e) {
+        const int mine = e * kThreads + (int)threadIdx.x, i = behind + (mine < all ? mine : all - 1);   // past the last: not stored
+        const int t = (int)by_token((unsigned)i), in = i - t * token_units, h = (int)by_units((unsigned)in);
+        unit[e] = in - h * units;
+        const bool half = PAIRS == Pairs::kHalves && unit[e] < turned;
+        const int d = (half || !kTwo ? unit[e] : 2 * unit[e]) * kVec;   // behind rot halves go on in twos
+        const size_t next = (size_t)(half ? pairs : kVec) * kEsize;
+        const bool key = h >= a.Hq;
+        const RotaryRows &r = key ? a.k : a.q;
+        const long long n = (long long)n0 + t, hh = key ? h - a.Hq : h;
+        const unsigned char *from = r.from + n * r.from_token + hh * r.from_head + (size_t)d * kEsize;
+        to[e] = r.to + n * r.to_token + hh * r.to_head + (size_t)d * kEsize, to2[e] = to[e] + next;
+        at[e] = mine < all ? t * pairs : -1;
+        x[e].load(from);
+        if (kTwo) y[e].load(from + next);
+    }
+    for (int i = (int)threadIdx.x; i < tokens * pairs; i += kThreads) {
+        const int t = (int)by_pairs((unsigned)i), p = i - t * pairs;
+        const float2 cs = turn(a.positions[(long long)n0 + t], a.freq[p]);
+        turns[i] = make_float2(cs.x * a.magnitude, cs.y * a.magnitude);
+    }
+    if constexpr (!kTwo) {   // whole heads: their units are a power of two, at most 32, and divide a batch
 #pragma unroll
-        for (int e = 0; e < kAhead; ++e) {
-            if (at[e] < 0) continue;
-            if (unit[e] < turned) {
+        for (int e = 0; e < AHEAD; ++e) x[e].store(lds + (e * kThreads + threadIdx.x) * 16);
+    }
+    __syncthreads();
 #pragma unroll
-                for (int v = 0; v < VEC; ++v) {
-                    const int p = unit[e] * VEC + v;
-                    if (INTER && p >= pairs) continue;
+    for (int e = 0; e < AHEAD; ++e) {
+        if (at[e] < 0 || unit[e] >= stored) continue;
+        if (unit[e] < turned) {
+            if constexpr (kTwo) {
+#pragma unroll
+                for (int v = 0; v < kVec; ++v) {
+                    const int p = unit[e] * kVec + v;
+                    if (kInter && p >= pairs) continue;
                     const float2 cs = turns[at[e] + p];
                     // elements 2v and 2v + 1 of the two pieces, or v of each
-                    P &first_of = INTER && 2 * v >= VEC ? y[e] : x[e], &second_of = !INTER || 2 * v + 1 >= VEC ? y[e] : x[e];
-                    const int ea = INTER ? (2 * v) % VEC : v, eb = INTER ? (2 * v + 1) % VEC : v;
+                    P &first_of = kInter && 2 * v >= kVec ? y[e] : x[e], &second_of = !kInter || 2 * v + 1 >= kVec ? y[e] : x[e];
+                    const int ea = kInter ? (2 * v) % kVec : v, eb = kInter ? (2 * v + 1) % kVec : v;
                     const float u = first_of.get(ea), w = second_of.get(eb);
                     first_of.set(ea, fmaf(u, cs.x, -(w * cs.y)));
                     second_of.set(eb, fmaf(w, cs.x, u * cs.y));
                 }
+            } else {
+                const unsigned char *head = lds + (e * kThreads + threadIdx.x - unit[e]) * 16;
+#pragma unroll
+                for (int v = 0; v < kVec; ++v) {
+                    const int d = unit[e] * kVec + v;
+                    if (d >= a.rot) continue;
+                    const bool low = d < pairs;
+                    const int other = low ? d + pairs : d - pairs;
+                    const float2 cs = turns[at[e] + (low ? d : other)];
+                    const float u = x[e].get(v);
+                    const float w = BF16 ? __uint_as_float((uint32_t)reinterpret_cast<const uint16_t *>(head)[other] << 16)
+                                         : reinterpret_cast<const float *>(head)[other];
+                    x[e].set(v, low ? fmaf(u, cs.x, -(w * cs.y)) : fmaf(u, cs.x, w * cs.y));
+                }
             }
-            x[e].store(to[e]), y[e].store(to2[e]);
         }
+        x[e].store(to[e]);
+        if (kTwo) y[e].store(to2[e]);
     }
 }
 
@@ -144,33 +168,35 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(Rotary a, int tokens, 
 
 hipError_t launch_rotary(const Rotary &a, int D, bool bf16, bool interleaved, hipStream_t stream)
 {
-    const int pairs = a.rot / 2;
-    // whole 16 bytes: a head's halves are apart by pairs elements, whose largest power of two
-    // that divides them a piece can have
-    int vec = bf16 ? 8 : 4;
-    while (!interleaved && pairs % vec) vec /= 2;
-    const int turned = (pairs + vec - 1) / vec;
+    const int pairs = a.rot / 2, vec = bf16 ? 8 : 4;
+    const Pairs how = interleaved ? Pairs::kInter : pairs % vec == 0 ? Pairs::kHalves : Pairs::kAnyHalf;
+    const int turned = how == Pairs::kAnyHalf ? (a.rot + vec - 1) / vec : (pairs + vec - 1) / vec;
     // in place nothing behind rot is touched
     const bool in_place = (a.Hq == 0 || a.q.from == a.q.to) && (a.Hkv == 0 || a.k.from == a.k.to);
-    const int units = in_place ? turned : D / (2 * vec), heads = a.Hq + a.Hkv;
-    if (units == 0) return hipSuccess;
-    const int tokens = a.N <= 2048 ? 1 : 4;
-    auto launch = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, wide_grid(((long long)a.N + tokens - 1) / tokens), dim3(kThreads),
-                           (size_t)tokens * (pairs ? pairs : 1) * sizeof(float2), stream, a, tokens, turned, make_div(units), units,
-                           make_div(heads), make_div(pairs ? pairs : 1));
+    const int whole = how == Pairs::kAnyHalf ? D / vec : D / (2 * vec), stored = in_place ? turned : whole;
+    const int units = how == Pairs::kAnyHalf ? whole : stored, token_units = (a.Hq + a.Hkv) * units;
+    if (stored == 0) return hipSuccess;
+    const long long total = (long long)a.N * token_units;
+    // a unit a lane until they fill the chip, then more; cosines and sines of at most 32 KB
+    const bool few = total <= 1024ll * kThreads;
+    const int most = 4096 / (pairs ? pairs : 1) - 2;   // tokens
+    int batch = (few ? 1 : kMany) * kThreads;
+    if (token_units * (long long)most < batch) batch = token_units * most;
+    const int tokens = batch / token_units + 2;
+    auto launch = [&](auto kernel, int ahead) {
+        const size_t lds = (size_t)tokens * pairs * sizeof(float2) + (how == Pairs::kAnyHalf ? ahead * kThreads * 16 : 0);
+        hipLaunchKernelGGL(kernel, wide_grid((total + batch - 1) / batch), dim3(kThreads), lds, stream, a, batch, turned, stored,
+                           make_div(token_units), token_units, make_div(units), units, make_div(pairs ? pairs : 1));
     };
-    if (interleaved) {
-        bf16 ? launch(rotary_kernel<true, 8, true>) : launch(rotary_kernel<false, 4, true>);
-    } else if (bf16) {
-        if (vec == 8) launch(rotary_kernel<true, 8, false>);
-        else if (vec == 4) launch(rotary_kernel<true, 4, false>);
-        else if (vec == 2) launch(rotary_kernel<true, 2, false>);
-        else launch(rotary_kernel<true, 1, false>);
-    } else {
-        if (vec == 4) launch(rotary_kernel<false, 4, false>);
-        else if (vec == 2) launch(rotary_kernel<false, 2, false>);
-        else launch(rotary_kernel<false, 1, false>);
+    auto of_type = [&](auto pairs_how) {
+        constexpr Pairs P = decltype(pairs_how)::value;
+        if (bf16) few ? launch(rotary_kernel<true, P, 1>, 1) : launch(rotary_kernel<true, P, kMany>, kMany);
+        else few ? launch(rotary_kernel<false, P, 1>, 1) : launch(rotary_kernel<false, P, kMany>, kMany);
+    };
+    switch (how) {
+    case Pairs::kInter: of_type(std::integral_constant<Pairs, Pairs::kInter>{}); break;
+    case Pairs::kHalves: of_type(std::integral_constant<Pairs, Pairs::kHalves>{}); break;
+    default: of_type(std::integral_constant<Pairs, Pairs::kAnyHalf>{}); break;
     }
     return hipGetLastError();
 }

@@ -60,7 +60,8 @@ def test_resize_rejects(kw, status, needle):
     (dict(N=-1), INVALID, "negative"), (dict(Hq=-1), INVALID, "negative"), (dict(Hkv=-1), INVALID, "negative"),
     (dict(D=48), UNSUPPORTED, "D=48"), (dict(dtype=2), UNSUPPORTED, "dtype"), (dict(rot=63), INVALID, "rot=63"),
     (dict(rot=66), INVALID, "rot=66"), (dict(rot=-2), INVALID, "rot=-2"), (dict(inter=2), INVALID, "interleaved=2"),
-    (dict(Hq=1 << 17), UNSUPPORTED, "2^17"), (dict(q=None), INVALID, "null"), (dict(k=None), INVALID, "null"),
+    (dict(Hq=1 << 17), UNSUPPORTED, "2^17"),
+    (dict(N=2**31 - 1, Hq=100, qt=6400, qot=6400), UNSUPPORTED, "too many tokens"), (dict(q=None), INVALID, "null"), (dict(k=None), INVALID, "null"),
     (dict(qo=None), INVALID, "null"), (dict(ko=None), INVALID, "null"), (dict(positions=None), INVALID, "null"),
     (dict(freq=None), INVALID, "null"), (dict(positions=3 * F + 2), INVALID, "aligned"), (dict(freq=4 * F + 4), INVALID, "aligned"),
     (dict(q=F + 8), INVALID, "16-byte"), (dict(ko=6 * F + 2), INVALID, "16-byte"), (dict(qt=260), INVALID, "multiples of 16"),
