@@ -182,15 +182,15 @@ __global__ __launch_bounds__(kRows) void resize_rows_kernel(PagedResize a, Div b
         if (!__syncthreads_or(cuts)) continue;
         const Scan at = block_scan((unsigned)cuts, part[0]);   // the table has at most INT_MAX entries
         cut[tid] = (int)at.before, keep[tid] = c.need;
-        const int all = (int)at.all;
+        const unsigned all = at.all;   // 2^31 - 1 at most; q0 may end behind that
         __syncthreads();
-        for (int q0 = 0; q0 < all; q0 += kAhead * kRows) {
+        for (unsigned q0 = 0; q0 < all; q0 += kAhead * kRows) {
             int pg[kAhead], *from[kAhead], i[kAhead], f[kAhead];
 #pragma unroll
             for (int e = 0; e < kAhead; ++e) {
-                const int q = q0 + e * kRows + tid;
+                const unsigned q = q0 + (unsigned)(e * kRows + tid);
                 pg[e] = q < all ? 0 : -1;
-                f[e] = all - 1 - (q < all ? q : all - 1);
+                f[e] = (int)(all - 1 - (q < all ? q : all - 1));
                 i[e] = 0;
             }
 #pragma unroll
@@ -218,7 +218,7 @@ __global__ __launch_bounds__(kRows) void resize_rows_kernel(PagedResize a, Div b
             }
 #pragma unroll
             for (int e = 0; e < kAhead; ++e) {
-                if (q0 + e * kRows + tid >= all) continue;
+                if (q0 + (unsigned)(e * kRows + tid) >= all) continue;
                 *from[e] = -1;
                 const int before = e * kParts + w;
                 const unsigned to = pushed + (before ? lane_of(sums[(before - 1) / kWave], (before - 1) % kWave) : 0) + (unsigned)__popcll(valid[e] & ((1ull << lane) - 1));

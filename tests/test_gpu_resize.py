@@ -125,6 +125,21 @@ def test_long_rows_and_large_calls():
     check(state(9, held, 16, 70, 200_000), held + rng.integers(0, 200, 5000), 16, 500_000, "5000 rows")
 
 
+def test_a_table_of_almost_2_to_the_31_entries_returned_at_once():
+    """Counts of returned pages step past 2^31 here."""
+    cols = 715_827_882
+    say(f"[resize] 3 rows of {cols} pages")
+    dev = device()
+    table = torch.full((3, cols), -1, dtype=I32, device=dev)
+    table[0, 0], table[1, 400_000_000], table[2, cols - 1] = 5, 7, 3
+    kv_len, free = torch.full((3,), cols, dtype=I32, device=dev), torch.full((8,), 9, dtype=I32, device=dev)
+    count = torch.zeros(1, dtype=I32, device=dev)
+    api.paged_resize(table, kv_len, torch.zeros(3, dtype=I32, device=dev), free, count, 1)
+    assert not kv_len.any() and count.item() == 3
+    assert free.tolist() == [3, 7, 5, 9, 9, 9, 9, 9]   # the last row's last page first
+    assert all(bool((row == -1).all()) for row in table)
+
+
 def test_outputs_that_are_not_asked_for_and_a_leading_dimension():
     d = state(10, [40, 0, 7], 16, 30, 60)
     for outputs in ((), ("start",), ("offsets", "slots"), ("positions",)):
