@@ -698,8 +698,8 @@ int fs_rotary_frequencies(double *freq, int rot, double base, double factor, int
  *                not touched)
  *   stream       hipStream_t (NULL = default stream)
  * Supported: dtype FS_F32 or FS_BF16, D in {16, 32, 64, 128}, rot even and <= D,
- * Hq + Hkv <= 2^17, pointers and strides of q, k and the outputs multiples of 16
- * bytes.
+ * Hq + Hkv <= 2^17, q and k of at most 2^42 bytes together, pointers and strides of q,
+ * k and the outputs multiples of 16 bytes.
  * Arithmetic: angles in fp64 and reduced there, cosines, sines, products and sums
  * in fp32, one rounding at the end.
  * Errors: FS_ERR_INVALID_ARG for negative sizes or strides, rot odd, negative or above

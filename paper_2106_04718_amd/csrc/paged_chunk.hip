@@ -4,9 +4,22 @@
 // i attends the positions up to kv_len - n + i in the key-value head h / G.  A row's queries
 // of one key-value head are n G columns, column m being head m % G of token m / G.
 //
-// Tiles.  A wave attends 32 positions for 16 NC columns at a time on the matrix cores, as
-// paged_tile.h describes, its four waves the positions in turn; their softmax states are
-// joined at the end.
+// Tiles.  A workgroup takes up to 128 columns (bf16, heads of 32 elements and more: wide), or 16 or
+// 32 (narrow).  In a narrow tile a wave attends 32 positions for all columns at a time, as
+// paged_tile.h describes, the four waves the positions in turn; their softmax states are
+// joined at the end.  In a wide one each wave has 32 columns and all positions, 64 of them at a
+// time, which the four read from LDS: from global memory straight to each wave's registers the
+// same keys would be asked for four times.
+// fp32 keeps to narrow tiles: 16 x 16 x 4 products of 32 columns a wave and all positions, the
+// caches serving four waves' loads, took 118 us where this takes 70 (8 rows of 1 to 257 tokens behind
+// 400 to 1024 positions, 16 heads of 64), and gained at one of five other sizes (272 -> 214 us).
+//
+// Bound.  A token of n over p positions has 4 p D operations, and a row's keys and values are read
+// once for all of its tokens and a key-value head's G heads: few tokens (32 rows of 5 over 200 to
+// 4096 positions, 285 MB: 78 us, 3.7 TB/s, 18 of them starting and joining) are bound by HBM, many by the
+// matrix cores and what stands between their products.  2048 tokens over 32500 positions, 32 heads
+// of 128: 1.40 to 1.51 ms, 700 to 755 TFLOP/s of 4 p D, of which the weights' second parts make half as
+// many again; the card's clock falls from 2.24 to 2.0 GHz meanwhile.
 //
 // Division of the work.  The columns of a row are cut into tiles.  Either workgroups take whole
 // tiles, the longest first; or all tiles of a key-value head, one behind another, are cut into
@@ -586,15 +599,15 @@ __device__ __forceinline__ void attend_wide(const PagedChunk &a, const Geo &geo,
         scale = scale == 0.f ? 1.f : fabsf(scale);
     }
 
-    // Lane l looks up position t0 + l of a tile, two tiles ahead of its use.
+    // Lane l looks up position t0 + l of a tile, two tiles ahead of its use.  Nothing is made of what
+    // is looked up before that, or the tile on its way, asked for earlier, would be waited for too.
     auto page_of = [&](int t0) {
         const int pos = t0 + lane;
-        const int pg = table[geo.by_page((unsigned)(pos < end ? pos : begin))];
-        return pos < end ? pg : -1;
+        return table[geo.by_page((unsigned)(pos < end ? pos : begin))];
     };
     auto load = [&](int buf, int t0, int pg) {   // asks for a tile; which of its positions there are
         const int pos = t0 + lane;
-        const bool ok = pg >= 0 && pg < c.pages;
+        const bool ok = pos < end && pg >= 0 && pg < c.pages;
         const unsigned off = ok ? slot16(a, geo, pg, pos) : 0u;
 #pragma unroll
         for (int i = 0; i < kDims; ++i) {
@@ -622,8 +635,12 @@ __device__ __forceinline__ void attend_wide(const PagedChunk &a, const Geo &geo,
     struct Values {
         bf16x8_t x[kDims];
     };
+    // Each weight is the sum of two bf16 values, within 2^-17 of it, so that the only rounding as coarse
+    // as the type's is the last.  2048 tokens over 32500 positions, in the first form of this kernel:
+    // one part 1238 us and 1.41 times the error of 32-bit weights rounded once at the end, two 1597 us,
+    // three 2000.
     struct Weights {
-        bf16x8_t hi, lo;   // each weight is the sum of the two
+        bf16x8_t hi, lo;
     };
     auto values = [&](const unsigned char *at, int s) {   // of 16 keys: 16 s + 4 h + 0 .. 3 and 8 behind
         Values r;
@@ -981,7 +998,7 @@ union Lds {
     JoinLds join;
 };
 
-// Waves a SIMD, and workgroups a CU: as many as the registers hold.
+// Waves a SIMD, and workgroups a CU: as many as the registers hold without spilling, and the LDS.
 constexpr int occupancy(int D, bool bf16) { return D <= (bf16 ? 64 : 32) ? 3 : 2; }
 
 template <int D, bool BF16>

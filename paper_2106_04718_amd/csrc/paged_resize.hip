@@ -9,7 +9,9 @@
 // kernel over the chip.
 //
 // Bound by latency: the first kernel is a chain of trips (lengths, returned pages, sums, taken
-// pages) on one CU, and the launches cost more than the bytes.
+// pages) on one CU, and the launches cost more than the bytes.  256 rows that take up to
+// 8 positions or give them back: 6 to 8 us; 1500 rows and some 280000 tokens: sums 21 to 25 us, pages and
+// slots 6.9.
 #include <limits.h>
 #include <stdint.h>
 

@@ -4,7 +4,8 @@
 //   a' = m (a cos - b sin),  b' = m (b cos + a sin)
 // (a, b) being elements (i, i + rot / 2) of the head or (2i, 2i + 1); elements from rot on
 // stay as they are.  Every element is read and written once, for some ten operations:
-// bound by HBM bandwidth.
+// bound by HBM bandwidth (16384 tokens of 40 bf16 heads of 128, 336 MB: 58 us, 5.7 TB/s; 5001 of 32 fp32
+// heads of 64, 82 MB: 18.7 us, 4.4 TB/s; a 1 GiB copy 5.1).
 //
 // The angle is taken in 64 bits, for far positions turn the first pairs through a million
 // radians (in 32 bits the angle of 2^20 is off by up to 0.03), and left by whole quarter
