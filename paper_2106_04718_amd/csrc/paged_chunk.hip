@@ -16,9 +16,9 @@
 //
 // Bound.  A token of n over p positions has 4 p D operations, and a row's keys and values are read
 // once for all of its tokens and a key-value head's G heads: few tokens (32 rows of 5 over 200 to
-// 4096 positions, 285 MB: 78 us, 3.7 TB/s, 18 of them starting and joining) are bound by HBM, many by the
+// 4096 positions, 285 MB: 74 us, 3.9 TB/s, 18 of them starting and joining) are bound by HBM, many by the
 // matrix cores and what stands between their products.  2048 tokens over 32500 positions, 32 heads
-// of 128: 1.40 to 1.51 ms, 700 to 755 TFLOP/s of 4 p D, of which the weights' second parts make half as
+// of 128: 1.40 to 1.46 ms, 725 to 755 TFLOP/s of 4 p D, of which the weights' second parts make half as
 // many again; the card's clock falls from 2.24 to 2.0 GHz meanwhile.
 //
 // Division of the work.  The columns of a row are cut into tiles.  Either workgroups take whole
@@ -529,7 +529,9 @@ __device__ __forceinline__ void attend_narrow(const PagedChunk &a, const Geo &ge
 template <int D>
 struct WideLds {
     static constexpr int kGroups = D / 8, kKeyGroup = 1024 + 16, kValueGroup = 1024 + 64;
-    unsigned char k[2][kGroups * kKeyGroup], v[2][kGroups * kValueGroup];
+    struct Rows {
+        unsigned char k[kGroups * kKeyGroup], v[kGroups * kValueGroup];
+    } tile[2];
     unsigned bad;   // whether a value of the tile is infinite or NaN, where that matters
     static __device__ __forceinline__ int value(int key) { return key % kGroups * kValueGroup + key / kGroups * (D * 2); }
 };
@@ -605,7 +607,9 @@ __device__ __forceinline__ void attend_wide(const PagedChunk &a, const Geo &geo,
         const int pos = t0 + lane;
         return table[geo.by_page((unsigned)(pos < end ? pos : begin))];
     };
-    auto load = [&](int buf, int t0, int pg) {   // asks for a tile; which of its positions there are
+    using Tile64 = typename Lds::Rows;
+    auto load = [&](const unsigned char *__restrict K, const unsigned char *__restrict V, Tile64 *__restrict to, int t0, int pg)
+                    __attribute__((always_inline)) {   // asks for a tile; which of its positions there are
         const int pos = t0 + lane;
         const bool ok = pos < end && pg >= 0 && pg < c.pages;
         const unsigned off = ok ? slot16(a, geo, pg, pos) : 0u;
@@ -613,8 +617,8 @@ __device__ __forceinline__ void attend_wide(const PagedChunk &a, const Geo &geo,
         for (int i = 0; i < kDims; ++i) {
             const int g = kDims * wave + i, key = lane / kGroups * kGroups + g;
             const size_t at = (size_t)(unsigned)__builtin_amdgcn_ds_bpermute(key << 2, (int)off) * 16 + lane % kGroups * 16;
-            copy16(Kh + at, lds.k[buf] + g * Lds::kKeyGroup);
-            copy16(Vh + at, lds.v[buf] + g * Lds::kValueGroup);
+            copy16(K + at, to->k + g * Lds::kKeyGroup);
+            copy16(V + at, to->v + g * Lds::kValueGroup);
         }
         return __ballot(ok);
     };
@@ -630,8 +634,8 @@ __device__ __forceinline__ void attend_wide(const PagedChunk &a, const Geo &geo,
 
     // operands: of K the lane's key n, of V^T its dim n of the keys 4 h + 0 .. 3, by a transposition
     // of the four keys that 16 lanes read
-    const unsigned char *k_at = lds.k[0] + n % kGroups * Lds::kKeyGroup + n / kGroups * (D * 2) + 16 * h;
-    const unsigned char *v_at = lds.v[0] + Lds::value(4 * h + (lane & 15) / 4) + 32 * ((lane >> 4) & 1) + 8 * (lane & 3);
+    const int k_at = n % kGroups * Lds::kKeyGroup + n / kGroups * (D * 2) + 16 * h;
+    const int v_at = Lds::value(4 * h + (lane & 15) / 4) + 32 * ((lane >> 4) & 1) + 8 * (lane & 3);
     struct Values {
         bf16x8_t x[kDims];
     };
@@ -655,8 +659,8 @@ __device__ __forceinline__ void attend_wide(const PagedChunk &a, const Geo &geo,
         }
         return r;
     };
-    auto attend = [&](int buf, int t0, unsigned long long live) {
-        const unsigned char *kt = k_at + buf * (int)sizeof lds.k[0], *vt = v_at + buf * (int)sizeof lds.v[0];
+    auto attend = [&](const Tile64 *now, int t0, unsigned long long live) __attribute__((always_inline)) {
+        const unsigned char *kt = now->k + k_at, *vt = now->v + v_at;
         f32x16_t sc[2];
         bf16x8_t kf[2][kSteps];
 #pragma unroll
@@ -775,13 +779,13 @@ __device__ __forceinline__ void attend_wide(const PagedChunk &a, const Geo &geo,
     // Values of positions that are not there become zeros: the loads brought anything.  And an
     // infinity or NaN would reach columns that do not attend its position, as 0 times it: such
     // elements are added to the columns that do and taken out.
-    auto tidy = [&](int buf, int t0, unsigned long long live) {
+    auto tidy = [&](Tile64 *now, int t0, unsigned long long live) __attribute__((always_inline)) {
         constexpr int kMine = kWideTile * D * 2 / 16 / kBlock;   // 16-byte pieces of a lane's
         bool bad = false;
 #pragma unroll
         for (int i = 0; i < kMine; ++i) {
             const int piece = tid + kBlock * i, key = piece / kGroups;
-            auto *x = reinterpret_cast<u32x4_t *>(lds.v[buf] + Lds::value(key) + piece % kGroups * 16);
+            auto *x = reinterpret_cast<u32x4_t *>(now->v + Lds::value(key) + piece % kGroups * 16);
             if (!(live >> key & 1)) {
                 *x = u32x4_t{0u, 0u, 0u, 0u};
             } else {
@@ -798,14 +802,14 @@ __device__ __forceinline__ void attend_wide(const PagedChunk &a, const Geo &geo,
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     const int dim = 32 * d + 8 * (i / 4) + 4 * h + i % 4;
-                    const float v = __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t *>(lds.v[buf] + Lds::value(key) + dim * 2) << 16);
+                    const float v = __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t *>(now->v + Lds::value(key) + dim * 2) << 16);
                     if (!(fabsf(v) < INFINITY) && t0 + key < lim) o[d][i] += v;
                 }
             }
         }
         __syncthreads();
         for (int i = tid; i < kWideTile * D; i += kBlock) {
-            auto *x = reinterpret_cast<uint16_t *>(lds.v[buf] + Lds::value(i / D)) + i % D;
+            auto *x = reinterpret_cast<uint16_t *>(now->v + Lds::value(i / D)) + i % D;
             if ((*x & 0x7f80u) == 0x7f80u) *x = 0;
         }
         if (tid == 0) lds.bad = 0u;
@@ -815,18 +819,28 @@ __device__ __forceinline__ void attend_wide(const PagedChunk &a, const Geo &geo,
     if (begin < end) {
         int pg = page_of(begin), buf = 0;
         int pg_next = page_of(end - begin > kWideTile ? begin + kWideTile : begin);
-        unsigned long long live = load(0, begin, pg), live_next = 0;
+        unsigned long long live = load(Kh, Vh, lds.tile, begin, pg);
         if (tid == 0) lds.bad = 0u;
         __builtin_amdgcn_s_waitcnt(0);
         __syncthreads();
-        for (int t0 = begin;; t0 += kWideTile, buf ^= 1, live = live_next) {
-            const bool more = end - t0 > kWideTile;
+        // Two tiles of one variable: that reads of `now` and the loads that go to `next` never meet is
+        // said by __restrict, or every read of LDS waits for all of these loads (32 rows of 5 tokens
+        // 78 us, 36 of 1 and 4 of 129 to 512 tokens 144; so 74 and 136).  Between steps everybody
+        // waits for them.
+        auto step = [&](const unsigned char *__restrict K, const unsigned char *__restrict V, Tile64 *__restrict now,
+                        Tile64 *__restrict next, int t0, bool more) __attribute__((always_inline)) {
+            unsigned long long live_next = 0;
             if (more) {
-                live_next = load(buf ^ 1, t0 + kWideTile, pg_next);
+                live_next = load(K, V, next, t0 + kWideTile, pg_next);
                 pg_next = page_of(end - t0 > 2 * kWideTile ? t0 + 2 * kWideTile : begin);
             }
-            if (t0 + kWideTile > w.seen || live != ~0ull) tidy(buf, t0, live);
-            if (t0 < last_lim) attend(buf, t0, live);
+            if (t0 + kWideTile > w.seen || live != ~0ull) tidy(now, t0, live);
+            if (t0 < last_lim) attend(now, t0, live);
+            live = live_next;
+        };
+        for (int t0 = begin;; t0 += kWideTile, buf ^= 1) {
+            const bool more = end - t0 > kWideTile;
+            step(Kh, Vh, lds.tile + buf, lds.tile + (buf ^ 1), t0, more);
             if (!more) break;
             __builtin_amdgcn_s_waitcnt(0);   // the next tile's rows have arrived, then everybody's
             __syncthreads();
@@ -1004,8 +1018,12 @@ constexpr int occupancy(int D, bool bf16) { return D <= (bf16 ? 64 : 32) ? 3 : 2
 template <int D, bool BF16>
 __global__ __launch_bounds__(kBlock, (occupancy(D, BF16))) void paged_chunk_kernel(PagedChunk a, Geo geo)
 {
-    __shared__ __align__(16) Lds<D, BF16> lds;
-    __shared__ Rows rows;
+    __shared__ __align__(16) struct {
+        Lds<D, BF16> lds;
+        Rows rows;
+    } shared;
+    Lds<D, BF16> &lds = shared.lds;
+    Rows &rows = shared.rows;
 
     const unsigned wg = wide_index();
     Piece p;
