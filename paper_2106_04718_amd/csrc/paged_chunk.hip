@@ -18,7 +18,7 @@
 // once for all of its tokens and a key-value head's G heads: few tokens (32 rows of 5 over 200 to
 // 4096 positions, 285 MB: 74 us, 3.9 TB/s, 18 of them starting and joining) are bound by HBM, many by the
 // matrix cores and what stands between their products.  2048 tokens over 32500 positions, 32 heads
-// of 128: 1.40 to 1.46 ms, 725 to 755 TFLOP/s of 4 p D, of which the weights' second parts make half as
+// of 128: 1.44 to 1.46 ms, 723 to 736 TFLOP/s of 4 p D, of which the weights' second parts make half as
 // many again; the card's clock falls from 2.24 to 2.0 GHz meanwhile.
 //
 // Division of the work.  The columns of a row are cut into tiles.  Either workgroups take whole
