@@ -735,7 +735,8 @@ size_t fs_paged_chunk_attn_workspace_bytes(int N, int R, int Hq, int Hkv, int pa
  * over the j < cols * page whose pg(j) lies in [0, P); out[n,h,:] = 0 where there is
  * none (p < 0 among them).  Nothing behind p reaches a token, infinities and NaN
  * included.  An infinite value among the attended ones gives an infinity or NaN.
- * With one token per row it is fs_paged_attn without k and v.  Tokens of no row
+ * With one token per row it is fs_paged_attn without k and v, but for the order of the sums.
+ * Tokens of no row
  * (before offsets[0], behind offsets[R]) are neither read nor written, so q and out
  * may be padded.
  *
@@ -753,9 +754,8 @@ size_t fs_paged_chunk_attn_workspace_bytes(int N, int R, int Hq, int Hkv, int pa
  *                replayed from graphs.
  *   stream       hipStream_t (NULL = default stream)
  * Supported: fs_paged_append's set; Hq a multiple of Hkv, N * Hq <= 2^28, R <= 2^24.
- * Arithmetic: products and sums in fp32, one rounding at the end; for a bf16 cache
- * each weight is the sum of two bf16 values, within 2^-17 of it.  The bits depend on the
- * data and the sizes, never on run or launch.
+ * Arithmetic: weights, products and sums in fp32, one rounding at the end.  The bits
+ * depend on the data and the sizes, never on run or launch.
  * Errors: those of fs_paged_attn for the arguments that both have.  N, R or Hq == 0
  * returns FS_OK with no launch.
  */

@@ -18,8 +18,7 @@
 // once for all of its tokens and a key-value head's G heads: few tokens (32 rows of 5 over 200 to
 // 4096 positions, 285 MB: 74 us, 3.9 TB/s, 18 of them starting and joining) are bound by HBM, many by the
 // matrix cores and what stands between their products.  2048 tokens over 32500 positions, 32 heads
-// of 128: 1.44 to 1.46 ms, 723 to 736 TFLOP/s of 4 p D, of which the weights' second parts make half as
-// many again; the card's clock falls from 2.24 to 2.0 GHz meanwhile.
+// of 128: 1.77 ms, 600 TFLOP/s of 4 p D, which the weights' second and third parts double.
 //
 // Division of the work.  The columns of a row are cut into tiles.  Either workgroups take whole
 // tiles, the longest first; or all tiles of a key-value head, one behind another, are cut into
@@ -56,8 +55,6 @@ template <int D, bool BF16>
 constexpr bool kHasWide = BF16 && D >= 32;
 
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
-typedef float f32x2_t __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
 constexpr int kSchedValu = 0x2, kSchedMfma = 0x8, kSchedRead = 0x100;   // kinds of instructions
 
@@ -639,12 +636,13 @@ __device__ __forceinline__ void attend_wide(const PagedChunk &a, const Geo &geo,
     struct Values {
         bf16x8_t x[kDims];
     };
-    // Each weight is the sum of two bf16 values, within 2^-17 of it, so that the only rounding as coarse
-    // as the type's is the last.  2048 tokens over 32500 positions, in the first form of this kernel:
-    // one part 1238 us and 1.41 times the error of 32-bit weights rounded once at the end, two 1597 us,
-    // three 2000.
+    // Each weight is the sum of three bf16 values, eight bits of it and a part, cut off: all its 24
+    // bits, so that the only rounding as coarse as the type's is the last.  With two parts, within 2^-17,
+    // 2.2 to 2.7 results in 1000 were not the bf16 value next to the exact one, with three 0.2 to
+    // 1.3 (2048 tokens over 32500 positions; elementary operations in 32 bits 1.9).  The third costs
+    // 1496 -> 1765 us there, 113 -> 131 for 512 tokens behind 7680, 73 -> 81 for 32 prompts of 1 to 1164.
     struct Weights {
-        bf16x8_t hi, lo;
+        bf16x8_t part[3];
     };
     auto values = [&](const unsigned char *at, int s) {   // of 16 keys: 16 s + 4 h + 0 .. 3 and 8 behind
         Values r;
@@ -737,20 +735,25 @@ __device__ __forceinline__ void attend_wide(const PagedChunk &a, const Geo &geo,
         float sum[2] = {0.f, 0.f};
         auto weights = [&](int s) {
             Weights r;
-            u32x4_t hi, lo;
+            u32x4_t part[3];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                f32x2_t p;
+                float p[2];
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
                     p[x] = __builtin_amdgcn_exp2f(fmaf(sc[s / 2][8 * (s % 2) + 2 * j + x], scale, -base));
                     sum[x] += p[x];
                 }
-                const uint32_t both = __builtin_bit_cast(uint32_t, __builtin_convertvector(p, bf16x2_t));
-                p[0] -= __uint_as_float(both << 16), p[1] -= __uint_as_float(both & 0xffff0000u);
-                hi[j] = both, lo[j] = __builtin_bit_cast(uint32_t, __builtin_convertvector(p, bf16x2_t));
+#pragma unroll
+                for (int i = 0; i < 3; ++i) {
+                    part[i][j] = __builtin_amdgcn_perm(__float_as_uint(p[1]), __float_as_uint(p[0]), 0x07060302u);
+#pragma unroll
+                    for (int x = 0; x < 2; ++x)
+                        if (i < 2) p[x] -= __uint_as_float(__float_as_uint(p[x]) & 0xffff0000u);
+                }
             }
-            r.hi = __builtin_bit_cast(bf16x8_t, hi), r.lo = __builtin_bit_cast(bf16x8_t, lo);
+#pragma unroll
+            for (int i = 0; i < 3; ++i) r.part[i] = __builtin_bit_cast(bf16x8_t, part[i]);
             return r;
         };
         Weights p = weights(0);
@@ -760,15 +763,16 @@ __device__ __forceinline__ void attend_wide(const PagedChunk &a, const Geo &geo,
             Weights p_next;
             if (s < 3) v_next = values(vt, s + 1), p_next = weights(s + 1);
 #pragma unroll
-            for (int d = 0; d < kDims; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v.x[d], p.hi, o[d], 0, 0, 0);
+            for (int i = 0; i < 3; ++i) {
 #pragma unroll
-            for (int d = 0; d < kDims; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v.x[d], p.lo, o[d], 0, 0, 0);
+                for (int d = 0; d < kDims; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v.x[d], p.part[i], o[d], 0, 0, 0);
+            }
             if (s < 3) {
 #pragma unroll
-                for (int d = 0; d < 2 * kDims; ++d) {
+                for (int d = 0; d < 3 * kDims; ++d) {
                     __builtin_amdgcn_sched_group_barrier(kSchedMfma, 1, 0);
                     __builtin_amdgcn_sched_group_barrier(kSchedRead, 1, 0);
-                    __builtin_amdgcn_sched_group_barrier(kSchedValu, 48 / (2 * kDims), 0);
+                    __builtin_amdgcn_sched_group_barrier(kSchedValu, 72 / (3 * kDims), 0);
                 }
                 v = v_next, p = p_next;
             }
