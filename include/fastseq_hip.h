@@ -754,8 +754,9 @@ size_t fs_paged_chunk_attn_workspace_bytes(int N, int R, int Hq, int Hkv, int pa
  *                replayed from graphs.
  *   stream       hipStream_t (NULL = default stream)
  * Supported: fs_paged_append's set; Hq a multiple of Hkv, N * Hq <= 2^28, R <= 2^24.
- * Arithmetic: weights, products and sums in fp32, one rounding at the end.  The bits
- * depend on the data and the sizes, never on run or launch.
+ * Arithmetic: weights, products and sums in fp32, one rounding at the end.  Scores may have
+ * any size that fp32 holds; sums of values, weighted by up to 2^9, have to lie within it too.
+ * The bits depend on the data and the sizes, never on run or launch.
  * Errors: those of fs_paged_attn for the arguments that both have.  N, R or Hq == 0
  * returns FS_OK with no launch.
  */

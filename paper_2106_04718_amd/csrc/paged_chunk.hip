@@ -626,7 +626,7 @@ __device__ __forceinline__ void attend_wide(const PagedChunk &a, const Geo &geo,
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
     }
-    float m = -INFINITY, l = 0.f;   // m: of the unscaled scores
+    float m = -INFINITY, l = 0.f;   // m: scaled
     bool any = false;
 
     // operands: of K the lane's key n, of V^T its dim n of the keys 4 h + 0 .. 3, by a transposition
@@ -719,19 +719,32 @@ __device__ __forceinline__ void attend_wide(const PagedChunk &a, const Geo &geo,
         {
             float lo, hi;
             lane_pair<32>(mx, lo, hi);
-            mx = fmaxf(lo, hi);
+            mx = fmaxf(lo, hi) * scale;
         }
         // Weights are taken relative to a maximum that may be left behind by up to 2^8: what has
         // been added up is scaled down seldom, and sums of 32 bits do not mind.
-        if (__any((mx - m) * scale > 8.f || m == -INFINITY)) {
+        if (__any(mx - m > 8.f || m == -INFINITY)) {
             const float top = fmaxf(m, mx);
-            const float f = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - top) * scale);   // nothing yet, but perhaps an infinity
+            const float f = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - top);   // nothing yet, but perhaps an infinity
             l *= f;
 #pragma unroll
             for (int d = 0; d < kDims; ++d) o[d] *= f;
             m = top;
         }
-        const float base = m == -INFINITY ? 0.f : m * scale;
+        const float base = m == -INFINITY ? 0.f : m;
+        // A score's product with the scale is not rounded before the maximum, which is, leaves it: a
+        // factor of all weights, of at most 2 where the maximum is below 2^24.  Above, where it would be
+        // any, these products are rounded too.
+        float factor = scale;
+        if (__any(fabsf(base) >= 0x1p24f)) {
+            const bool far = fabsf(base) >= 0x1p24f;
+            factor = far ? 1.f : scale;
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sc[b][i] *= far ? scale : 1.f;
+            }
+        }
         float sum[2] = {0.f, 0.f};
         auto weights = [&](int s) {
             Weights r;
@@ -741,7 +754,7 @@ __device__ __forceinline__ void attend_wide(const PagedChunk &a, const Geo &geo,
                 float p[2];
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
-                    p[x] = __builtin_amdgcn_exp2f(fmaf(sc[s / 2][8 * (s % 2) + 2 * j + x], scale, -base));
+                    p[x] = __builtin_amdgcn_exp2f(fmaf(sc[s / 2][8 * (s % 2) + 2 * j + x], factor, -base));
                     sum[x] += p[x];
                 }
 #pragma unroll
@@ -861,7 +874,7 @@ __device__ __forceinline__ void attend_wide(const PagedChunk &a, const Geo &geo,
         if (w.parts == 1) {
             write_wide<D>(w.out + w.place<D>(a, geo, cc, 4 * h) * 2, o, any ? l : -1.f);
         } else if (h == 0) {
-            put(w.record + geo.width * D + 2 * cc, m * scale), put(w.record + geo.width * D + 2 * cc + 1, any ? l : -1.f);
+            put(w.record + geo.width * D + 2 * cc, m), put(w.record + geo.width * D + 2 * cc + 1, any ? l : -1.f);
         }
     }
     if (w.parts > 1 && mine > 0) {   // as the registers hold them, so that a wave's stores lie side by side

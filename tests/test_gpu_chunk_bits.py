@@ -53,3 +53,44 @@ def test_weights_keep_their_bits_where_values_cancel(D, R, T, behind):
     # bits are off by up to 64 of w c, half of the terms.
     tol = 2.0 ** -8 * np.abs(want) + 20 * 2.0 ** -24 * terms
     assert (np.abs(got - want) <= tol).all(), np.max((np.abs(got - want) - 2.0 ** -8 * np.abs(want)) / (2.0 ** -24 * terms))
+
+
+@pytest.mark.parametrize("low", [False, True])
+@pytest.mark.parametrize("dtype,D", [(BF16, 16), (BF16, 32), (BF16, 64), (BF16, 128), (torch.float32, 64)])
+@pytest.mark.parametrize("T,behind", [(1, 40), (40, 260), (200, 0), (5, 9000), (90, 6000)])
+def test_equal_scores_of_any_size_weigh_alike(T, behind, dtype, D, low):
+    """Scores far above 2^24, positive or negative: every third position has the largest, alike in all of
+    them, and the others a score so much lower that their weight is 0.  Rows of two kinds in one
+    call: their scores differ in size."""
+    R, Hkv, G, page = 3, 2, 4, 16
+    rng = np.random.default_rng(D + T)
+    L = behind + T
+    cols = -(-L // page)
+    size = bf16(np.array([30000.0, 9000.0, 1.0]))
+    best, other = (-1.0, -1.25) if low else (1.0, 0.75)
+    q = np.ones((R, T, Hkv * G, D)) * size[:, None, None, None]
+    at = np.arange(cols * page).reshape(cols, 1, page, 1)
+    K = np.where(at % 3 == 0, best, other) * size[:, None, None, None, None] * np.ones((R, cols, Hkv, page, D))
+    K[2] = best   # small scores, every one of them alike
+    V = bf16(rng.standard_normal((R, cols, Hkv, page, D)))
+    dev = device()
+    t = lambda x: torch.from_numpy(x).float().to(dtype).to(dev)
+    i = lambda x: torch.tensor(x, dtype=torch.int32, device=dev)
+    for scale in (D ** -0.5, -0.3):
+        say(f"[chunk bits] equal scores D={D} T={T} behind={behind} low={low} scale={scale} {dtype}")
+        out = api.paged_chunk_attn(t(q if scale > 0 else -q).view(R * T, Hkv * G, D), t(K).view(R * cols, Hkv, page, D),
+                                   t(V).view(R * cols, Hkv, page, D), i(np.arange(R * cols).reshape(R, cols)), i([L] * R),
+                                   i(np.arange(R + 1) * T), scale=scale)
+        got = out.double().cpu().numpy().reshape(R, T, Hkv, G, D)
+        v = V.transpose(0, 2, 1, 3, 4).reshape(R, Hkv, cols * page, D)
+        for r in range(R):
+            every = 3 if r < 2 else 1
+            for n in range(T):
+                seen = v[r, :, :behind + n + 1:every]
+                want, mean = seen.mean(1)[:, None], np.abs(seen).mean(1)[:, None]
+                # half a step of the type and what sums of fp32 lose of as many terms, of values and of
+                # weights; the weights of small scores of 1.45 D 0.3 at most in base 2, times the
+                # rounding of both, are alike in all
+                tol = (2.0 ** -8 if dtype == BF16 else 2.0 ** -24) * np.abs(want) + 2 * (seen.shape[1] + 64) * 2.0 ** -24 * mean
+                err = np.abs(got[r, n] - want)
+                assert (err <= tol).all(), (r, n, np.max(err / tol))
