@@ -744,7 +744,8 @@ size_t fs_paged_chunk_attn_workspace_bytes(int N, int R, int Hq, int Hkv, int pa
  *   q            [N, Hq, D] dtype, strides q_token_stride and q_head_stride
  *   K, V, table  as for fs_paged_append; only read
  *   kv_len       [R] int32, the row's new tokens included
- *   offsets      [R + 1] int32, not decreasing
+ *   offsets      [R + 1] int32, not decreasing; offsets[R] may be more than N, as
+ *                fs_paged_resize may leave it: tokens behind the N have their positions, no more
  *   scale        as for fs_paged_attn
  *   out          [N, Hq, D] dtype, contiguous
  *   workspace, workspace_bytes  at least fs_paged_chunk_attn_workspace_bytes bytes,

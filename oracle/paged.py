@@ -149,7 +149,7 @@ def paged_chunk_attn(q, K, V, table, kv_len, offsets, scale=None):
     cap = table.shape[1] * page
     for r in range(table.shape[0]):
         lo, hi = int(offsets[r]), int(offsets[r + 1])
-        for n in range(lo, hi):
+        for n in range(max(lo, 0), min(hi, N)):
             p = max(int(kv_len[r]), 0) - hi + n
             out[n] = 0
             slots = [s for s in (_slot(table, r, j, page, P) for j in range(min(p + 1, cap))) if s is not None]

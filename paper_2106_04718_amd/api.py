@@ -799,7 +799,7 @@ def paged_chunk_attn(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, table: t
     (``offsets`` [R + 1] int32); K, V [P, Hkv, page, D] and table [R, cols] as for
     :func:`paged_append`, Hq a multiple of Hkv; kv_len [R] int32, the positions of each
     row, its new tokens' included, whose keys and values the cache holds already.  A token
-    attends the positions up to its own.  ``scale`` (default 1 / sqrt(D)) multiplies the
+    attends the positions up to its own; a row's tokens behind the N have theirs, no more.  ``scale`` (default 1 / sqrt(D)) multiplies the
     scores.  Returns out [N, Hq, D] in the input dtype; zeros where a token attends
     nothing.  Tokens of no row are left as they are (uninitialised in an ``out`` made here).
     """

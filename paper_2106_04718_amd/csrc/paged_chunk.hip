@@ -83,10 +83,11 @@ struct Row {
 __device__ __forceinline__ int units_of(int L) { return L <= 0 ? 1 : (L + kUnit - 1) / kUnit; }
 
 __device__ __forceinline__ Row row_of(const PagedChunk &a, const Geo &geo, int kv_len, int o0, int o1) {
-    o0 = o0 < 0 ? 0 : o0, o1 = o1 < a.N ? o1 : a.N;   // of tokens that there are
-    const int n = o1 > o0 ? o1 - o0 : 0, L = kv_len < 0 ? 0 : kv_len;
+    o0 = o0 < 0 ? 0 : o0;
+    const int last = o1 < a.N ? o1 : a.N;   // of tokens that there are
+    const int n = last > o0 ? last - o0 : 0, L = kv_len < 0 ? 0 : kv_len;
     Row w;
-    w.first_pos = L - n;
+    w.first_pos = L - (n ? o1 - o0 : 0);   // those behind the N have their positions too
     w.begin = o0, w.tokens = n;
     w.columns = n * geo.G;
     w.tiles = (int)(((unsigned)w.columns + geo.width - 1) >> (31 - __builtin_clz(geo.width)));
@@ -150,7 +151,8 @@ __device__ __forceinline__ void add_rows(const PagedChunk &a, const Geo &geo, Ro
     for (int i = 0; i < 4; ++i) {
         const Row w = row_of(a, geo, len[i], off[i], off[i + 1]);   // none behind the last row: it would begin at its end
         work[i] = work_before(a, geo, w, w.tiles), sum += work[i];
-        const int u = w.tiles ? units_of(len[i] < cap ? len[i] : cap) : 0;
+        const int seen = w.first_pos + w.tokens;   // by its last token
+        const int u = w.tiles ? units_of(seen < cap ? seen : cap) : 0;
         longest = longest > u ? longest : u, tiles[i] = w.tiles, all_tiles += w.tiles;
         rows.len[4 * lane + i] = len[i], rows.off[4 * lane + i] = off[i];
     }
