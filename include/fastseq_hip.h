@@ -629,7 +629,8 @@ size_t fs_paged_resize_workspace_bytes(int R, int N);
  *     row is granted if W <= cols * page and it needs no page, or the pages that
  *     it and the rows before it need (those with W <= cols * page) are there.
  * kv_len[r] becomes W where the row shrank, stayed or was granted, and is left as it
- * was, like its pages, where it was refused.
+ * was, like its pages, where it was refused; the table's entries for the pages that it
+ * wanted become -1.
  *
  * The tokens to be added, A = max(0, W - L) of each row (granted or not), are
  * numbered row by row:
@@ -639,7 +640,10 @@ size_t fs_paged_resize_workspace_bytes(int R, int N);
  *     slots[n] = table[r, positions[n] / page] * page + positions[n] % page
  * slots[n] is -1 where the row was refused or its page is none of [0, P).
  * Entries of no token get position 0 and slot -1.  start and offsets are what
- * fs_paged_append takes, positions what fs_rotary takes.
+ * fs_paged_append takes, positions what fs_rotary takes.  A refused row's tokens are
+ * numbered too: fs_paged_append writes those that fall into the row's last page, behind its
+ * end, and no others; fs_paged_chunk_attn takes them for the last of the positions that the
+ * row holds, so what it gives for them is of no use, and touches no other row's.
  *
  * Arguments (device pointers except the sizes):
  *   table        [R, cols] int32, leading dimension ld_table >= cols

@@ -105,6 +105,8 @@ def paged_resize(table, kv_len, want, free_pages, free_count, page, N=0):
                 count -= 1
                 table[r, j] = free[count]
             kv_len[r] = wants[r]
+        elif more > 0:
+            table[r, pages(held[r]):pages(wants[r])] = -1
     off = [0]
     for r in range(R):
         off.append(off[-1] + max(0, wants[r] - held[r]))

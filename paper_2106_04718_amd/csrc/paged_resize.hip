@@ -257,6 +257,12 @@ __global__ __launch_bounds__(kRows) void resize_rows_kernel(PagedResize a, Div b
             if constexpr (ALL) held_of[tid] = h, wanted_of[tid] = (int)before, offset_of[tid + 1] = end;
             else s.held[r] = h, s.wanted[r] = (int)before, s.offsets[r + 1] = end;
         }
+        // Nothing is taken by a refused row's tokens: its table names no page where they would lie
+        for (unsigned long long left = __ballot(!ok && c.need > c.has); left; left &= left - 1) {
+            const int from = __ffsll((long long)left) - 1, row = b * kRows + w * kWave + from;
+            const int behind = (int)lane_of((unsigned)c.has, from), need = (int)lane_of((unsigned)c.need, from);
+            for (int j = behind + lane; j < need && j < a.cols; j += kWave) a.table[(size_t)row * a.ld_table + j] = -1;
+        }
         wanted = add_up(wanted, x.all), tokens = add_up(tokens, y.all);
     }
     __syncthreads();
