@@ -698,8 +698,8 @@ int fs_rotary_frequencies(double *freq, int rot, double base, double factor, int
  *   positions    [N] int32
  *   freq         [rot / 2] fp64, radians a position
  *   q_out, k_out as q and k, with strides of their own; q_out may be q and k_out
- *                k, with the same strides (in place: elements from rot on are then
- *                not touched)
+ *                k, with the same strides (in place: elements from rot on of that array
+ *                are then not written, so another stream may write them meanwhile)
  *   stream       hipStream_t (NULL = default stream)
  * Supported: dtype FS_F32 or FS_BF16, D in {16, 32, 64, 128}, rot even and <= D,
  * Hq + Hkv <= 2^17, q and k of at most 2^42 bytes together, pointers and strides of q,

@@ -55,6 +55,14 @@ struct Piece {
         w = __builtin_nontemporal_load(reinterpret_cast<const words_t *>(p));
     }
     __device__ __forceinline__ void store(unsigned char *p) const { *reinterpret_cast<words_t *>(p) = w; }
+    // its first n elements, an even number
+    __device__ __forceinline__ void store(unsigned char *p, int n) const {
+        constexpr int kOfWord = BF16 ? 2 : 1;
+        if (n >= 4 * kOfWord) return store(p);
+        if (n >= 2 * kOfWord) *reinterpret_cast<uint64_t *>(p) = (uint64_t)w[1] << 32 | w[0];
+        if (n >= 3 * kOfWord) reinterpret_cast<uint32_t *>(p)[2] = w[2];
+        else if (n >= kOfWord && n < 2 * kOfWord) reinterpret_cast<uint32_t *>(p)[0] = w[0];
+    }
     __device__ __forceinline__ float get(int e) const {
         if constexpr (!BF16) return __uint_as_float(w[e]);
         else return __uint_as_float(e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
@@ -77,10 +85,11 @@ struct Piece {
 // elements behind rot too); the others are copied.  Units are numbered along all tokens and heads,
 // and a workgroup has `batch` of them, AHEAD a lane, whose loads are on their way together: with
 // whole tokens a workgroup instead, some lanes would go round more often than others (9000
-// tokens of 72 heads of 128, 332 MB, 73 us; 16384 of 40 64).  In place nothing behind `turned`
-// is stored.
+// tokens of 72 heads of 128, 332 MB, 73 us; 16384 of 40 64).  In place nothing from element rot
+// on is stored, for another stream may write there meanwhile (9000 tokens of 72 bf16 heads of 128, 20
+// elements interleaved: 44 us, where whole units take 32).
 enum class Pairs { kInter, kHalves, kAnyHalf };
-template <bool BF16, Pairs PAIRS, int AHEAD>
+template <bool BF16, Pairs PAIRS, int AHEAD, bool PARTLY>   // PARTLY: in place, and a unit goes past rot or may
 __global__ __launch_bounds__(kThreads) void rotary_kernel(Rotary a, int batch, int turned, int stored, Div by_token, int token_units,
                                                           Div by_units, int units, Div by_pairs)
 {
@@ -99,7 +108,7 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(Rotary a, int batch, i
 
     P x[AHEAD], y[AHEAD];
     unsigned char *to[AHEAD], *to2[AHEAD];
-    int at[AHEAD], unit[AHEAD];
+    int at[AHEAD], unit[AHEAD], left[AHEAD];   // left: elements that are stored, from the unit's first on
 #pragma unroll
     for (int e = 0; e < AHEAD; ++e) {
         const int mine = e * kThreads + (int)threadIdx.x, i = behind + (mine < all ? mine : all - 1);   // past the last: not stored
@@ -114,6 +123,7 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(Rotary a, int batch, i
         const unsigned char *from = r.from + n * r.from_token + hh * r.from_head + (size_t)d * kEsize;
         to[e] = r.to + n * r.to_token + hh * r.to_head + (size_t)d * kEsize, to2[e] = to[e] + next;
         at[e] = mine < all ? t * pairs : -1;
+        left[e] = PARTLY && r.from == r.to && !half ? a.rot - d : 2 * kVec;
         x[e].load(from);
         if (kTwo) y[e].load(from + next);
     }
@@ -160,8 +170,8 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(Rotary a, int batch, i
                 }
             }
         }
-        x[e].store(to[e]);
-        if (kTwo) y[e].store(to2[e]);
+        x[e].store(to[e], left[e]);
+        if (kTwo) y[e].store(to2[e], left[e] - kVec);
     }
 }
 
@@ -174,6 +184,8 @@ hipError_t launch_rotary(const Rotary &a, int D, bool bf16, bool interleaved, hi
     const int turned = how == Pairs::kAnyHalf ? (a.rot + vec - 1) / vec : (pairs + vec - 1) / vec;
     // in place nothing behind rot is touched
     const bool in_place = (a.Hq == 0 || a.q.from == a.q.to) && (a.Hkv == 0 || a.k.from == a.k.to);
+    const bool either = (a.Hq > 0 && a.q.from == a.q.to) || (a.Hkv > 0 && a.k.from == a.k.to);
+    const bool partly = in_place ? a.rot % (how == Pairs::kInter ? 2 * vec : how == Pairs::kAnyHalf ? vec : 2) != 0 : either;
     const int whole = how == Pairs::kAnyHalf ? D / vec : D / (2 * vec), stored = in_place ? turned : whole;
     const int units = how == Pairs::kAnyHalf ? whole : stored, token_units = (a.Hq + a.Hkv) * units;
     if (stored == 0) return hipSuccess;
@@ -191,8 +203,12 @@ hipError_t launch_rotary(const Rotary &a, int D, bool bf16, bool interleaved, hi
     };
     auto of_type = [&](auto pairs_how) {
         constexpr Pairs P = decltype(pairs_how)::value;
-        if (bf16) few ? launch(rotary_kernel<true, P, 1>, 1) : launch(rotary_kernel<true, P, kMany>, kMany);
-        else few ? launch(rotary_kernel<false, P, 1>, 1) : launch(rotary_kernel<false, P, kMany>, kMany);
+        auto of_place = [&](auto some) {
+            constexpr bool PARTLY = decltype(some)::value;
+            if (bf16) few ? launch(rotary_kernel<true, P, 1, PARTLY>, 1) : launch(rotary_kernel<true, P, kMany, PARTLY>, kMany);
+            else few ? launch(rotary_kernel<false, P, 1, PARTLY>, 1) : launch(rotary_kernel<false, P, kMany, PARTLY>, kMany);
+        };
+        partly ? of_place(std::true_type{}) : of_place(std::false_type{});
     };
     switch (how) {
     case Pairs::kInter: of_type(std::integral_constant<Pairs, Pairs::kInter>{}); break;
