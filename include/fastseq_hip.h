@@ -71,9 +71,10 @@
  *     other calls on the same workspace.
  *   - Debug mode: with the environment variable FS_VALIDATE=1 set when the
  *     library is first used (or after fs_set_tuning(FS_TUNE_VALIDATE, 1)),
- *     the attention calls copy src_len / prefix_len / kv_len
+ *     the attention calls copy src_len / prefix_len / kv_len and offsets
  *     to the host (synchronising `stream`) and return FS_ERR_INVALID_ARG if
- *     a length lies outside [0, S] instead of clamping it; on a capturing
+ *     a length lies outside [0, S] instead of clamping it, or if the
+ *     offsets decrease; on a capturing
  *     stream, where that copy cannot run, they return FS_ERR_UNSUPPORTED.
  */
 #ifndef FASTSEQ_HIP_H

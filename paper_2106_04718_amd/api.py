@@ -236,8 +236,9 @@ def attn_path(name: str):
 
 @contextlib.contextmanager
 def validate_lengths(on: bool = True):
-    """Debug mode inside the block: the attention calls copy the lengths to
-    the host and reject out-of-range ones (FS_VALIDATE)."""
+    """Debug mode inside the block: the attention calls copy the lengths and
+    offsets to the host and reject out-of-range lengths and offsets that
+    decrease (FS_VALIDATE)."""
     prev = set_tuning(_N.FS_TUNE_VALIDATE, int(on))
     try:
         yield

@@ -113,16 +113,30 @@ unsigned long long attn_epoch(hipStream_t s, fs::AttnPath path) {
 // FS_VALIDATE's check of the device-resident lengths: a synchronous copy to
 // the host, refused while the stream is capturing (the copy and the
 // synchronisation would end the capture).
-int validate_lengths(const int32_t *len, int B, int limit, hipStream_t s, const char *what) {
+int copy_to_host(std::vector<int32_t> &to, const int32_t *from, hipStream_t s, const char *what) {
     if (capturing(s))
         return fail(FS_ERR_UNSUPPORTED, "FS_VALIDATE copies %s to the host, which a capturing stream cannot do", what);
-    std::vector<int32_t> lens((size_t)B);
-    hipError_t e = hipMemcpyAsync(lens.data(), len, (size_t)B * 4, hipMemcpyDeviceToHost, s);
+    hipError_t e = hipMemcpyAsync(to.data(), from, to.size() * 4, hipMemcpyDeviceToHost, s);
     if (e == hipSuccess) e = hipStreamSynchronize(s);
     if (e != hipSuccess) return fail(FS_ERR_HIP, "FS_VALIDATE copy of %s: %s (%d)", what, hipGetErrorString(e), (int)e);
+    return FS_OK;
+}
+int validate_lengths(const int32_t *len, int B, int limit, hipStream_t s, const char *what) {
+    std::vector<int32_t> lens((size_t)B);
+    const int st = copy_to_host(lens, len, s, what);
+    if (st != FS_OK) return st;
     for (int b = 0; b < B; ++b)
         if (lens[b] < 0 || lens[b] > limit)
             return fail(FS_ERR_INVALID_ARG, "%s[%d] = %d outside [0, %d]", what, b, lens[b], limit);
+    return FS_OK;
+}
+// The same for running sums of n numbers that are not negative.
+int validate_offsets(const int32_t *offsets, int n, hipStream_t s, const char *what) {
+    std::vector<int32_t> at((size_t)n + 1);
+    const int st = copy_to_host(at, offsets, s, what);
+    if (st != FS_OK) return st;
+    for (int i = 0; i < n; ++i)
+        if (at[i] > at[i + 1]) return fail(FS_ERR_INVALID_ARG, "%s[%d] = %d is above %s[%d] = %d", what, i, at[i], what, i + 1, at[i + 1]);
     return FS_OK;
 }
 
@@ -1146,7 +1160,9 @@ int fs_paged_chunk_attn(const void *q, int64_t q_token_stride, int64_t q_head_st
     if (overlaps(workspace, need, out, out_bytes)) return fail(FS_ERR_INVALID_ARG, "workspace overlaps an argument");
 
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (validate_mode() && (st = validate_lengths(kv_len, R, cols * page, s, "kv_len")) != FS_OK) return st;
+    if (validate_mode() && ((st = validate_lengths(kv_len, R, cols * page, s, "kv_len")) != FS_OK ||
+                            (st = validate_offsets(offsets, R, s, "offsets")) != FS_OK))
+        return st;
     fs::PagedChunk a{};
     a.cache = paged_cache(const_cast<void *>(K), const_cast<void *>(V), page_stride, head_stride, slot_stride, P, page, table,
                           ld_table, cols, esize);
