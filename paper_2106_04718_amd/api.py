@@ -784,12 +784,8 @@ def rotary(q: torch.Tensor, positions: torch.Tensor, freq: torch.Tensor, k: torc
 def paged_chunk_attn_workspace_bytes(N: int, R: int, Hq: int, Hkv: int, page: int, cols: int, D: int,
                                      dtype: torch.dtype = torch.bfloat16) -> int:
     """Bytes of workspace fs_paged_chunk_attn needs for these sizes (cols: the table's columns)."""
-    key = ("c", N, R, Hq, Hkv, page, cols, D, dtype)
-    n = _WS_BYTES.get(key)
-    if n is None:
-        n = _size_or_raise(_native_lib().fs_paged_chunk_attn_workspace_bytes(N, R, Hq, Hkv, page, cols, D, _DTYPES[dtype]))
-        _WS_BYTES[key] = n
-    return n
+    # not kept, as other calls' are: N is another one in every step of a server
+    return _size_or_raise(_native_lib().fs_paged_chunk_attn_workspace_bytes(N, R, Hq, Hkv, page, cols, D, _DTYPES[dtype]))
 
 
 def paged_chunk_attn(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, table: torch.Tensor, kv_len: torch.Tensor,
