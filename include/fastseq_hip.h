@@ -645,6 +645,8 @@ size_t fs_paged_resize_workspace_bytes(int R, int N);
  * numbered too: fs_paged_append writes those that fall into the row's last page, behind its
  * end, and no others; fs_paged_chunk_attn takes them for the last of the positions that the
  * row holds, so what it gives for them is of no use, and touches no other row's.
+ * fs_paged_attn with k and v would write over the last of these positions: where pages may
+ * not last, it is given lengths of 0 for rows whose kv_len is not what was wanted.
  *
  * Arguments (device pointers except the sizes):
  *   table        [R, cols] int32, leading dimension ld_table >= cols

@@ -662,7 +662,8 @@ def paged_resize(table: torch.Tensor, kv_len: torch.Tensor, want: torch.Tensor, 
     free_pages [P] int32, a stack of the ``free_count`` ([1] int32) pages that are
     free.  Rows that shrink give their pages back, then rows that grow take theirs, in
     their order, while there are enough; kv_len of a row that gets none stays as it was, and
-    its tokens have no slots.
+    its tokens have no slots (:func:`paged_attn` with k and v then has to be given a length of
+    0 for it, ``torch.where(kv_len == want, kv_len, 0)``).
     Optional outputs: start [R] int32, the positions held before; offsets [R + 1] int32,
     the running sums of the tokens added; positions [N] int32 and slots [N] int64, of
     every token its position and its slot of the cache (page id times ``page`` and the

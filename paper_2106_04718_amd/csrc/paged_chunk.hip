@@ -1031,7 +1031,8 @@ union Lds {
     JoinLds join;
 };
 
-// Waves a SIMD, and workgroups a CU: as many as the registers hold without spilling, and the LDS.
+// Waves a SIMD, and workgroups a CU: as many as the registers and the LDS hold.  bf16 heads of 64 spill
+// 6 registers, 28 bytes a lane, at 3: 32 prompts of 1 to 1164 tokens of 12 heads take 81 us, with 2 93.
 constexpr int occupancy(int D, bool bf16) { return D <= (bf16 ? 64 : 32) ? 3 : 2; }
 
 template <int D, bool BF16>

@@ -56,3 +56,27 @@ def test_appended_tokens_of_refused_rows_stay_in_their_last_page():
         want[4] = want[2, 0] = True         # the granted row's tokens
         want[3, 10:] = True                 # behind the end of the second row, in its last page
         assert torch.equal(wrote, want)
+
+
+def test_a_refused_rows_token_left_out_of_the_attention_of_one_token():
+    """Lengths of 0 for rows that got no page: nothing of theirs is written, and their results are 0."""
+    dev = device()
+    Hq, Hkv, D, page, P = 4, 2, 64, 16, 6
+    g = torch.Generator(device=dev).manual_seed(2)
+    r = lambda *s: torch.randn(*s, device=dev, generator=g).bfloat16()
+    i = lambda *a: torch.tensor(a, dtype=I32, device=dev)
+    K, V = r(P, Hkv, page, D), r(P, Hkv, page, D)
+    keep = K.clone(), V.clone()
+    table = torch.full((3, 4), -1, dtype=I32, device=dev)
+    table[0, 0], table[1, 0], table[2, 0] = 0, 3, 5
+    kv_len, free, count = i(16, 16, 9), i(4, 0, 0, 0, 0, 0), i(1)
+    want = kv_len + 1
+    api.paged_resize(table, kv_len, want, free, count, page)
+    say("[resize refused] one token")
+    q, k, v = r(3, Hq, D), r(3, Hkv, D), r(3, Hkv, D)
+    out = api.paged_attn(q, K, V, table, torch.where(kv_len == want, kv_len, 0), k=k, v=v)
+    torch.cuda.synchronize()
+    assert kv_len.tolist() == [17, 16, 10] and not out[1].any() and out[0].any() and out[2].any()
+    for C, was, x in ((K, keep[0], k), (V, keep[1], v)):
+        was[4, :, 0], was[5, :, 9] = x[0], x[2]
+        assert torch.equal(C, was)
