@@ -16,9 +16,10 @@
 //
 // Bound.  A token of n over p positions has 4 p D operations, and a row's keys and values are read
 // once for all of its tokens and a key-value head's G heads: few tokens (32 rows of 5 over 200 to
-// 4096 positions, 285 MB: 74 us, 3.9 TB/s, 18 of them starting and joining) are bound by HBM, many by the
+// 4096 positions, 285 MB: 75 us, 3.8 TB/s) are bound by HBM, many by the
 // matrix cores and what stands between their products.  2048 tokens over 32500 positions, 32 heads
-// of 128: 1.77 ms, 600 TFLOP/s of 4 p D, which the weights' second and third parts double.
+// of 128: 1.76 to 1.85 ms, 573 to 601 TFLOP/s of 4 p D, which the weights' second and third parts double;
+// the matrix cores are busy 57 % of the cycles.
 //
 // Division of the work.  The columns of a row are cut into tiles.  Either workgroups take whole
 // tiles, the longest first; or all tiles of a key-value head, one behind another, are cut into
@@ -844,7 +845,7 @@ __device__ __forceinline__ void attend_wide(const PagedChunk &a, const Geo &geo,
         __syncthreads();
         // Two tiles of one variable: that reads of `now` and the loads that go to `next` never meet is
         // said by __restrict, or every read of LDS waits for all of these loads (32 rows of 5 tokens
-        // 78 us, 36 of 1 and 4 of 129 to 512 tokens 144; so 74 and 136).  Between steps everybody
+        // 78 us, 36 of 1 and 4 of 129 to 512 tokens 144; so 74 and 136; weights of two parts).  Between steps everybody
         // waits for them.
         auto step = [&](const unsigned char *__restrict K, const unsigned char *__restrict V, Tile64 *__restrict now,
                         Tile64 *__restrict next, int t0, bool more) __attribute__((always_inline)) {
@@ -1059,8 +1060,8 @@ __global__ __launch_bounds__(kBlock, (occupancy(D, BF16))) void paged_chunk_kern
     u64_t share = (all + (unsigned)geo.shares - 1) / (unsigned)geo.shares;
     // Whole tiles take the longest's time or the mean of the shares.  Cut ones take that, a part's
     // record and the joining, and wide ones find less of their keys in the L2 (us, whole and cut: 2048
-    // tokens over 32500 positions 1436 and 1618, 32 prompts of 1 to 1164 tokens 75 and 87;
-    // 32 rows of 5 tokens over 200 to 4096 167 and 74, 512 tokens over 8192 262 and 121).
+    // tokens over 32500 positions 1844 and 1849, 32 prompts of 1 to 1164 tokens 81 and 91, 8 of 1 to 257
+    // in fp32 71 and 75; 32 rows of 5 tokens over 200 to 4096 127 and 75, 512 tokens over 8192 249 and 133).
     bool whole = false;
     if (!geo.plan) {
         const float mean = (float)share, longest = (float)(rows.longest * kUnit + kStart);
